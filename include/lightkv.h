@@ -26,6 +26,12 @@
  * survivors are emitted in their original order (Step 5).  The same map is
  * applied to the layer's K/V cache, which the method shrinks together with the
  * tokens (appendix "Method overview").
+ *
+ * Behind the prefill the library serves the caches that the method left: page
+ * numbers and slots for growing and shrunken requests (lightkv_assign_pages),
+ * the rows of new tokens (lightkv_append_kv) and the attention of one new token
+ * per request (lightkv_decode_attention).  These take their sizes with every
+ * call and need no plan.
  */
 #ifndef LIGHTKV_H_
 #define LIGHTKV_H_
@@ -54,7 +60,10 @@ extern "C" {
 #define LIGHTKV_STATUS_TIMEOUT     4u   /* a bounded device-side wait expired                  */
 #define LIGHTKV_STATUS_COUNT       8u   /* a sample holds more tokens, A / B nodes or survivors
                                            than the stage's capacities: its tokens pass through
-                                           unmerged, cut at cap_out                              */
+                                           unmerged, cut at cap_out; serving calls: more tokens
+                                           than a block table or a slot map has room for         */
+#define LIGHTKV_STATUS_PAGE       16u   /* a page number or a slot outside the pool: its row was left out */
+#define LIGHTKV_STATUS_NO_PAGES   32u   /* the free pages did not suffice: requests kept their old length */
 
 /* storage / arithmetic type of hidden states, Q, K, V */
 #define LIGHTKV_BF16 0   /* bf16 storage, fp32 accumulation                     */
@@ -328,6 +337,119 @@ typedef struct {
 } lightkv_kv_args_t;
 
 int lightkv_compact_kv(const lightkv_plan_t* plan, const lightkv_kv_args_t* args);
+
+/* ---- serving a compacted cache ------------------------------------------------------------------------------------------
+ * A paged cache is a pool of n_pages pages of page_size rows for each of K and V, addressed as for lightkv_compact_kv; the
+ * slot of token n of request b is block_table[b][n / page_size] * page_size + n % page_size. */
+
+/* Bring block tables in line with the requests' lengths and list the slots of the new tokens.
+ *   held   h_b = max(held[b], 0) tokens, whose ceil(h_b / page_size) pages stand in the table (held = NULL: none)
+ *   wanted w_b = seq_len[b] + add tokens; a negative seq_len[b] marks a place of the batch without a request: w_b = 0
+ * Requests with fewer pages wanted than held give the last ones back, requests with more get the missing ones:
+ *   - the pages given back are pushed on the stack free_pages[0 .. n_free), request by request, a request's in table order
+ *     (their table entries stay as they are);
+ *   - then the missing ones are popped from its top, request by request.  A request is served while the pages asked for up to
+ *     and including it do not exceed the stack; from the first that is not served on, no further one that asks for pages is:
+ *     these keep their pages and their h_b tokens, and raise LIGHTKV_STATUS_NO_PAGES.
+ * A request that wants more than max_blocks * page_size tokens is not served either (LIGHTKV_STATUS_COUNT); lengths held beyond
+ * that, or an n_free outside [0, n_pages], are cut to it and raise the same bit.  Entries of block_table and free_pages must be
+ * page numbers that occur once; one outside [0, n_pages) is passed on as it is, its tokens get no slot (LIGHTKV_STATUS_PAGE).
+ * seq_len_out[b] is w_b, h_b for a request that was not served, and seq_len[b] for a place without a request.
+ * Slots: request b has max(w_b - h_b, 0) new tokens, served or not; slot_start[b] is their number in front of b.  The i-th one's
+ * slot goes to slot_map[slot_start[b] + i], or, with slot_stride > 0, to slot_map[b * slot_stride + i] where i < slot_stride.
+ * Every other entry of slot_map [n_slots], those of requests not served among them, becomes -1.  Tokens for whose slots there
+ * is no room raise LIGHTKV_STATUS_COUNT.
+ * seq_len_out may be the array held or seq_len, n_free_out the word n_free; everything else is disjoint. */
+typedef struct {
+  uint32_t struct_size;            /* sizeof(lightkv_pages_args_t) */
+  int32_t  batch;
+  int32_t  page_size, max_blocks;  /* max_blocks: row stride of block_table */
+  int32_t  n_pages;                /* pages of the pool, room of free_pages */
+  int32_t  add;                    /* >= 0 */
+  const int32_t* held;             /* DEVICE [B] or NULL */
+  const int32_t* seq_len;          /* DEVICE [B] */
+  int32_t* seq_len_out;            /* DEVICE [B] */
+  int32_t* block_table;            /* DEVICE [B, max_blocks] */
+  int32_t* free_pages;             /* DEVICE [n_pages] */
+  const int32_t* n_free;           /* DEVICE, one word */
+  int32_t* n_free_out;             /* DEVICE, one word */
+  int64_t* slot_map;               /* DEVICE [n_slots] or NULL */
+  int32_t  n_slots, slot_stride;
+  int32_t* slot_start;             /* DEVICE [B + 1] or NULL (numbers beyond 2^31 - 1 are cut to it) */
+  uint32_t* status;                /* DEVICE, OR-ed into; may be NULL */
+  void*    workspace;              /* DEVICE, 256-byte aligned */
+  size_t   workspace_bytes;
+  void*    stream;
+} lightkv_pages_args_t;
+
+/* Bytes of scratch lightkv_assign_pages needs for `batch` requests; HOST only.  0 for a negative batch. */
+size_t lightkv_pages_workspace(int32_t batch);
+/* Errors: INVALID_ARG (NULL or overlapping buffers, sizes that are not positive, slot_stride without a slot map, ...), WORKSPACE. */
+int lightkv_assign_pages(const lightkv_pages_args_t* args);
+
+/* Write the key and value rows of n_tokens new tokens to their slots of a paged cache; all heads of token t go to slot
+ * slot_map[t].  A contiguous cache [B, H_kv, N, dh] is one with n_pages = B and page_size = N.  Negative slots are skipped
+ * silently, slots behind the pool with LIGHTKV_STATUS_PAGE.  Slots must differ; of two equal ones either row may stand there
+ * afterwards.  Sources and caches are disjoint. */
+typedef struct {
+  uint32_t struct_size;            /* sizeof(lightkv_append_args_t) */
+  int32_t  n_tokens;               /* >= 0 */
+  int32_t  n_kv_heads, head_dim;   /* head_dim: multiple of 8, at most 256 */
+  int32_t  dtype;                  /* LIGHTKV_BF16 | LIGHTKV_FP32 */
+  int32_t  page_size, n_pages;
+  const void* k_new; const void* v_new;      /* DEVICE [n_tokens, H_kv, dh] */
+  int64_t  new_token_stride, new_head_stride;
+  void* k_cache; void* v_cache;              /* DEVICE */
+  int64_t  page_stride, head_stride, row_stride;
+  const int64_t* slot_map;         /* DEVICE [n_tokens] */
+  uint32_t* status;                /* DEVICE, may be NULL */
+  void*    stream;
+} lightkv_append_args_t;
+
+int lightkv_append_kv(const lightkv_append_args_t* args);
+
+/* Attention of one new token per request over the request's cache, grouped heads:
+ *   out[b, h] = sum_j p_j V[b, h / (H / H_kv), j],  p = softmax_j(scale q[b, h] . K[b, h / (H / H_kv), j]),  j < n_keys[b]
+ *   lse[b, h] = log sum_j exp(scale q . K_j)
+ * computed in one pass over K and V.  Logits, sums and the accumulated rows are fp32; bf16 rows are rounded once, at the end.
+ * A request with n_keys[b] <= 0 has a row of zeros and lse = -inf, and so has one whose logits are all -inf.
+ * k_new, v_new: rows of the token itself.  They stand for row n_keys[b] - 1 of the cache and are written there by the call.
+ * Keys whose page number lies outside [0, n_pages) are left out (LIGHTKV_STATUS_PAGE); n_keys beyond the table's (or a
+ * contiguous request's) rows is cut to them (LIGHTKV_STATUS_COUNT).  What the cache holds behind n_keys[b] is not read.
+ * The workspace need not be cleared and may be shared by calls that are ordered on the device. */
+typedef struct {
+  uint32_t struct_size;            /* sizeof(lightkv_decode_args_t) */
+  int32_t  batch;
+  int32_t  n_q_heads, n_kv_heads;  /* H, H_kv; H % H_kv == 0 */
+  int32_t  head_dim;               /* multiple of 8, at most 256 */
+  int32_t  dtype;                  /* LIGHTKV_BF16 | LIGHTKV_FP32 */
+  float    scale;                  /* 0: 1 / sqrt(head_dim) */
+  int32_t  page_size;              /* 0: contiguous, request b's rows start b * page_stride into the caches */
+  int32_t  max_blocks;             /* row stride of block_table (paged) */
+  int32_t  n_pages;                /* pages of the pool (paged) */
+  int32_t  max_keys;               /* contiguous: rows of a request.  Paged: an upper bound of n_keys that the caller knows, or
+                                      0; it only helps to choose how the work is split */
+  const void* q;                   /* DEVICE [B, H, dh] */
+  int64_t  q_batch_stride, q_head_stride;
+  void* k_cache; void* v_cache;    /* DEVICE; written only where k_new is given */
+  int64_t  page_stride, head_stride, row_stride;
+  const int32_t* block_table;      /* DEVICE [B, max_blocks] (paged) */
+  const int32_t* n_keys;           /* DEVICE [B] */
+  const void* k_new; const void* v_new;      /* DEVICE [B, H_kv, dh], both or neither */
+  int64_t  new_batch_stride, new_head_stride;
+  void*    out;                    /* DEVICE [B, H, dh]; does not overlap q */
+  int64_t  out_batch_stride, out_head_stride;
+  float*   lse;                    /* DEVICE [B, H] or NULL */
+  int64_t  lse_batch_stride, lse_head_stride;
+  uint32_t* status;                /* DEVICE, may be NULL */
+  void*    workspace;              /* DEVICE, 256-byte aligned */
+  size_t   workspace_bytes;
+  void*    stream;
+} lightkv_decode_args_t;
+
+/* Bytes of scratch lightkv_decode_attention needs for these sizes, whatever the lengths; HOST only.  0 for sizes it refuses. */
+size_t lightkv_decode_workspace(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype);
+int lightkv_decode_attention(const lightkv_decode_args_t* args);
 
 const char* lightkv_status_string(int status);
 int lightkv_version(void);

@@ -92,9 +92,43 @@ class _KvArgs(C.Structure):
                 ("src_seq_start", C.c_void_p), ("dst_seq_start", C.c_void_p)]
 
 
+class _PagesArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("batch", C.c_int32), ("page_size", C.c_int32), ("max_blocks", C.c_int32),
+                ("n_pages", C.c_int32), ("add", C.c_int32), ("held", C.c_void_p), ("seq_len", C.c_void_p),
+                ("seq_len_out", C.c_void_p), ("block_table", C.c_void_p), ("free_pages", C.c_void_p),
+                ("n_free", C.c_void_p), ("n_free_out", C.c_void_p), ("slot_map", C.c_void_p), ("n_slots", C.c_int32),
+                ("slot_stride", C.c_int32), ("slot_start", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+class _AppendArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("k_new", C.c_void_p),
+                ("v_new", C.c_void_p), ("new_token_stride", C.c_int64), ("new_head_stride", C.c_int64),
+                ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("row_stride", C.c_int64), ("slot_map", C.c_void_p), ("status", C.c_void_p), ("stream", C.c_void_p)]
+
+
+class _DecodeArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("page_size", C.c_int32),
+                ("max_blocks", C.c_int32), ("n_pages", C.c_int32), ("max_keys", C.c_int32), ("q", C.c_void_p),
+                ("q_batch_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64), ("block_table", C.c_void_p),
+                ("n_keys", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("new_batch_stride", C.c_int64),
+                ("new_head_stride", C.c_int64), ("out", C.c_void_p), ("out_batch_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("lse", C.c_void_p), ("lse_batch_stride", C.c_int64),
+                ("lse_head_stride", C.c_int64), ("status", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
+
+
+# bits of a call's status word
+STATUS_POS_ORDER, STATUS_ZERO_WEIGHT, STATUS_TIMEOUT, STATUS_COUNT, STATUS_PAGE, STATUS_NO_PAGES = 1, 2, 4, 8, 16, 32
+
 EXPORTS = ("lightkv_plan", "lightkv_plan_stage_info", "lightkv_plan_destroy", "lightkv_plan_retention",
            "lightkv_compress_layer", "lightkv_compress_layer_builtin_ws", "lightkv_compact_kv",
-           "lightkv_status_string", "lightkv_version")
+           "lightkv_decode_workspace", "lightkv_decode_attention", "lightkv_append_kv", "lightkv_pages_workspace",
+           "lightkv_assign_pages", "lightkv_status_string", "lightkv_version")
 BUILTIN_WS_BYTES = 8 << 20
 
 
@@ -124,6 +158,13 @@ def library() -> C.CDLL:
         lib.lightkv_compress_layer_builtin_ws.restype = C.c_int
         lib.lightkv_compact_kv.argtypes = [C.c_void_p, C.POINTER(_KvArgs)]
         lib.lightkv_compact_kv.restype = C.c_int
+        lib.lightkv_decode_workspace.argtypes = [C.c_int32] * 5
+        lib.lightkv_decode_workspace.restype = C.c_size_t
+        lib.lightkv_pages_workspace.argtypes = [C.c_int32]
+        lib.lightkv_pages_workspace.restype = C.c_size_t
+        for name, struct in (("decode_attention", _DecodeArgs), ("append_kv", _AppendArgs), ("assign_pages", _PagesArgs)):
+            entry = getattr(lib, "lightkv_" + name)
+            entry.argtypes, entry.restype = [C.POINTER(struct)], C.c_int
         lib.lightkv_status_string.argtypes = [C.c_int]
         lib.lightkv_status_string.restype = C.c_char_p
         lib.lightkv_version.argtypes = []
@@ -244,9 +285,11 @@ def _binding():
         except ImportError as exc:
             raise LightKVError(f"_binding.so is missing: build it first (python -c 'import __graft_entry__ as g; g.build()'): {exc}")
         address = lambda f: C.cast(f, C.c_void_p).value
-        native.bind(address(lib.lightkv_compress_layer), address(lib.lightkv_compress_layer_builtin_ws),
-                    address(lib.lightkv_compact_kv), _fail, _fork_join, torch._C._cuda_getCurrentRawStream,
-                    torch.cuda.current_device)
+        native.bind(tuple(address(f) for f in (lib.lightkv_compress_layer, lib.lightkv_compress_layer_builtin_ws,
+                                               lib.lightkv_compact_kv, lib.lightkv_decode_attention, lib.lightkv_append_kv,
+                                               lib.lightkv_assign_pages)),
+                    _fail, _fork_join, torch._C._cuda_getCurrentRawStream, torch.cuda.current_device,
+                    (torch.bfloat16, torch.float32, torch.int32, torch.int64))
         _BINDING = native
     return _BINDING
 
@@ -277,3 +320,42 @@ def compact_kv(plan: Plan, stage: int, out: StageBuffers, k_src, v_src, k_dst, v
     Paged: k/v page pools [n_pages, H_kv, page_size, dh] views and int32 block tables [B, max_blocks]."""
     (_BINDING or _binding()).compact_kv(plan, stage, out, k_src, v_src, k_dst, v_dst, vis_begin, n_text_after, mode, n_vis,
                                         page_size, src_block_table, dst_block_table, stream, src_seq_start, dst_seq_start)
+
+
+def decode_workspace_bytes(batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int = BF16) -> int:
+    """Bytes of the workspace tensor decode_attention wants (with room to align it)."""
+    n = library().lightkv_decode_workspace(batch, n_q_heads, n_kv_heads, head_dim, dtype)
+    if n == 0:
+        raise LightKVError("lightkv_decode_workspace: invalid argument")
+    return n + 256
+
+
+def pages_workspace_bytes(batch: int) -> int:
+    """Bytes of the workspace tensor assign_pages wants (with room to align it)."""
+    n = library().lightkv_pages_workspace(batch)
+    if n == 0:
+        raise LightKVError("lightkv_pages_workspace: invalid argument")
+    return n + 256
+
+
+def decode_attention(q, k_cache, v_cache, n_keys, out, **kw) -> None:
+    """lightkv_decode_attention.  q, out [B,H,dh]; n_keys [B] int32.  With block_table [B,max_blocks] int32 the caches are
+    page pools [n_pages,H_kv,page_size,dh], else [B,H_kv,N,dh] (any strides with a contiguous last dimension, the same for K
+    and V).  Keywords: workspace (required: a tensor of decode_workspace_bytes bytes), lse [B,H] fp32, k_new / v_new
+    [B,H_kv,dh] (rows that stand for key n_keys - 1 and are written to the cache), scale (default 1 / sqrt(dh)), max_keys (an
+    upper bound of n_keys, paged), status [1] int32, stream.  All tensors are on the current device."""
+    (_BINDING or _binding()).decode_attention(q, k_cache, v_cache, n_keys, out, **kw)
+
+
+def append_kv(k_new, v_new, k_cache, v_cache, slot_map, **kw) -> None:
+    """lightkv_append_kv.  k_new, v_new [T,H_kv,dh]; caches [n_pages,H_kv,page_size,dh]; slot_map [T] int64, negative: skipped.
+    Keywords: status [1] int32, stream."""
+    (_BINDING or _binding()).append_kv(k_new, v_new, k_cache, v_cache, slot_map, **kw)
+
+
+def assign_pages(seq_len, block_table, free_pages, n_free, **kw) -> None:
+    """lightkv_assign_pages.  seq_len [B] int32, block_table [B,max_blocks] int32, free_pages [n_pages] int32, n_free [1] int32.
+    Keywords: page_size and workspace (required; a tensor of pages_workspace_bytes bytes), add, held [B] int32, seq_len_out [B]
+    (default: in place of held, or of seq_len where none is given), n_free_out [1] (default: in place of n_free), slot_map
+    [n_slots] int64, slot_start [B+1] int32, slot_stride, status [1] int32, stream."""
+    (_BINDING or _binding()).assign_pages(seq_len, block_table, free_pages, n_free, **kw)
