@@ -3,28 +3,30 @@
 //   out = softmax(scale q K^T) V  per (request, query head),  lse = log sum exp(scale q K^T)
 //
 // Every key and value is read once and used for two dot products per query head, so the pass is bound by HBM wherever the
-// query heads of a key head share the read.  A warp walks its own pieces of 16 keys and keeps the running maximum and sum of
-// the softmax; nothing is shared between warps before the end, and nothing between lanes before the dot products: each lane
-// copies (cp.async) the 16-byte pieces that it will itself need as MMA fragments into a ring of its own and reads them back,
-// without a barrier or a shuffle.
+// query heads of a key head share the read.  A warp walks its own pieces of 16 keys through its own ring of cp.async stages and
+// keeps the running maximum and sum of the softmax; no barrier stands between warps before the end.  What has to be kept
+// low is the latency of a piece's arithmetic: a warp that computes longer than its ring's copies take leaves HBM idle.
 //
 // bf16: keys are the rows of the first product (S^T = K Q^T, mma.sync m16n8k16: 16 keys x 8 query heads), channels the rows of
-// the second (O^T = V^T P^T).  The order of the channels inside a dot product and of the keys inside a sum is free, so a lane's
-// fragments are whole 16-byte pieces of its rows: K rows lane / 4 and lane / 4 + 8, V rows 2 (lane % 4) + {0, 1, 8, 9}, whose
-// 16-bit halves are paired up by byte permutes.  P is rounded to two bf16 summands (hi + lo, 16 bits of mantissa): with one
-// the rounding of P would be as large as the rounding of the output row.
-// tcgen05 would need 64 rows of query heads, or V transposed through shared memory, to save arithmetic that HBM hides.
+// the second (O^T = V^T P^T), so that eight query heads fill the narrow side of an MMA.  Rows lie in shared memory as they
+// come, 16-byte units permuted by the row's last three bits; ldmatrix reads K as it is and V transposed.  P is rounded to two
+// bf16 summands (hi + lo, 16 bits of mantissa): with one the rounding of P would be as large as the rounding of the output row.
+// tcgen05 would need 64 rows of query heads to save arithmetic that HBM hides.
 #include <math.h>
 
+#include <algorithm>
+
 #include "launch.h"
+#include "tc_common.cuh"
 
 namespace lkv {
 
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kTile = 32;              // keys whose rows a warp looks up at once, one per lane
-constexpr int kPiece = 16;             // keys of a ring stage
+constexpr int kSms = 148;              // the workspace is sized for them
+constexpr int kMaxCluster = 8;
+constexpr int kPiece = 16;             // keys of a ring stage; a warp looks up the rows of two pieces at once, one per lane
 
 struct DecodeArgs {
   const char* q; const char* k; const char* v; const char* k_new; const char* v_new;
@@ -33,32 +35,42 @@ struct DecodeArgs {
   const int* table;                    // nullptr: contiguous
   const int* n_keys;
   uint32_t* status;
-  // strides in bytes (lse: elements)
-  int64_t q_batch, q_head, page, head, row, new_batch, new_head, out_batch, out_head, lse_batch, lse_head;
+  int64_t lse_batch, lse_head;         // elements
+  // strides in units of 16 bytes
+  uint32_t q_batch, q_head, page, head, row, new_batch, new_head, out_batch, out_head;
   int n_kv_heads, group, row_blocks, dh, page_size, max_blocks, n_pages;
-  long long cap;                       // rows a request has room for
+  int cap;                             // rows a request has room for
   float scale_log2;
+  unsigned page_mul; int page_shift;   // key / page_size = (umulhi(key, page_mul) + key) >> page_shift for key < 2^31
+  int aligned;                         // pieces do not straddle pages
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 bytes, the first `bytes` of them from global memory, the rest zero
+using tc::cluster_sync;
+using tc::smem_u32;
+
+// i strides of 16-byte units, in bytes
+__device__ __forceinline__ int64_t bytes_of(uint32_t i, uint32_t stride) { return int64_t((uint64_t(i) * stride) << 4); }
+// 16 bytes, the first `bytes` of them from global memory, the rest zero; TO, FROM: constant offsets
+template <int TO, int FROM>
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+  asm volatile("cp.async.cg.shared.global [%0+%3], [%1+%4], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(TO), "n"(FROM) : "memory");
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
+// f(Const<0>) ... f(Const<N - 1>)
+template <int I> struct Const { static constexpr int value = I; };
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+  if constexpr (I < N) {
+    f(Const<I>());
+    unrolled<N, I + 1>(f);
+  }
 }
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 __device__ __forceinline__ float exp2_approx(float x) {
@@ -66,122 +78,203 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// What a warp knows of one request and key head.
+// What a warp knows of one request and key head, and of the piece whose rows are looked up.
 struct Walk {
   const char *k, *v;                   // the head's row 0 of page 0
   const char *k_new, *v_new;           // rows that stand for key n - 1, or nullptr
   const int* table;
   int n;                               // keys
-  int page_no;                         // page of this lane's key of the tile that is looked up next (-1: none)
-  int64_t off;                         // bytes to its row, of the tile in hand
-  unsigned mask;                       // bit i: key i of the tile in hand is there
+  int first, step;                     // pieces first, first + step, ...
+  // Page numbers are asked for long before they are needed.  Aligned: lane i holds that of the (32 j + i)-th piece, `ahead` those of
+  // the next 32.  Else lanes 0 .. 15 hold those of the keys of an even piece, 16 .. 31 of the one behind it, `ahead` of the next two.
+  int pages, ahead;
+  int64_t off;                         // bytes to the row of key lane % 16 (aligned: of key 0) of the piece in hand
+  unsigned mask;                       // bit i: key i of the piece in hand is there
+  int own;                             // which of them the token's own row stands for, or -1
   bool bad;                            // a page number outside the pool was met
 
-  // page number of this lane's key of tile t
-  __device__ __forceinline__ int page_of(const DecodeArgs& a, int t, int limit) const {
-    const unsigned key = unsigned(t) * kTile + (threadIdx.x & 31);
-    if (key >= unsigned(limit)) return -1;
-    return table ? table[key / unsigned(a.page_size)] : 0;
-  }
-  // rows of tile t, whose page numbers are in page_no
-  __device__ __forceinline__ void locate(const DecodeArgs& a, int t) {
-    const unsigned key = unsigned(t) * kTile + (threadIdx.x & 31);
-    bool ok = key < unsigned(n);
-    if (table) {
-      const bool in_pool = unsigned(page_no) < unsigned(a.n_pages);
-      bad |= ok && !in_pool;
-      ok = ok && in_pool;
-      off = ok ? int64_t(page_no) * a.page + int64_t(key % unsigned(a.page_size)) * a.row : 0;
-    } else {
-      off = ok ? int64_t(key) * a.row : 0;
+  __device__ __forceinline__ void start(const DecodeArgs& a, int b, int hk, int first_piece, int by) {
+    table = a.table ? a.table + size_t(b) * a.max_blocks : nullptr;
+    const int64_t at = bytes_of(hk, a.head) + (a.table ? 0 : bytes_of(b, a.page));
+    k = a.k + at;
+    v = a.v + at;
+    k_new = v_new = nullptr;
+    if (a.k_new) {
+      const int64_t own_at = bytes_of(b, a.new_batch) + bytes_of(hk, a.new_head);
+      k_new = a.k_new + own_at;
+      v_new = a.v_new + own_at;
     }
-    mask = __ballot_sync(0xffffffffu, ok);
+    first = first_piece; step = by;
+    bad = false;
+  }
+  static __device__ __forceinline__ unsigned block_of(const DecodeArgs& a, unsigned key) { return (__umulhi(key, a.page_mul) + key) >> a.page_shift; }
+  // this lane's page number among those looked up from the i-th piece on; -1 behind `limit` keys
+  __device__ __forceinline__ int look_up(const DecodeArgs& a, int i, int limit) const {
+    const unsigned lane = threadIdx.x & 31;
+    const long long piece = first + (long long)(i + int(a.aligned ? lane : lane >> 4)) * step;
+    const long long key = piece * kPiece + (a.aligned ? 0 : lane & 15);
+    return key < limit ? table[block_of(a, unsigned(key))] : -1;
+  }
+  __device__ __forceinline__ void look(const DecodeArgs& a, int limit) {
+    if (!table) return;
+    pages = look_up(a, 0, limit);
+    ahead = look_up(a, a.aligned ? 32 : 2, limit);
+  }
+  // rows of the i-th piece; called for i = 0, 1, 2, ...
+  __device__ __forceinline__ void locate(const DecodeArgs& a, int i) {
+    const unsigned lane = threadIdx.x & 31, key0 = unsigned(first + i * step) * kPiece, there = unsigned(n) - key0;
+    mask = there >= kPiece ? 0xffffu : (1u << there) - 1u;
+    own = k_new && there <= unsigned(kPiece) ? int(there) - 1 : -1;
+    if (!table) {
+      off = bytes_of(key0, a.row);
+    } else if (a.aligned) {
+      const int page = __shfl_sync(0xffffffffu, pages, i & 31);
+      const bool in_pool = unsigned(page) < unsigned(a.n_pages);
+      if (!in_pool) { mask = 0; bad = true; }
+      off = in_pool ? bytes_of(page, a.page) + bytes_of(key0 - block_of(a, key0) * unsigned(a.page_size), a.row) : 0;
+      if ((i & 31) == 31) {
+        pages = ahead;
+        ahead = look_up(a, i + 33, n);
+      }
+    } else {
+      const int page = __shfl_sync(0xffffffffu, pages, (i & 1) * 16 + (lane & 15));
+      const unsigned key = key0 + (lane & 15);
+      const bool in_pool = unsigned(page) < unsigned(a.n_pages), ok = key < unsigned(n);
+      bad |= ok && !in_pool;
+      mask &= __ballot_sync(0xffffffffu, in_pool);
+      off = ok && in_pool ? bytes_of(page, a.page) + bytes_of(key - block_of(a, key) * unsigned(a.page_size), a.row) : 0;
+      if (i & 1) {
+        pages = ahead;
+        ahead = look_up(a, i + 3, n);
+      }
+    }
   }
 };
 
+// fp32, K: rows are copied in whole lines, 32 consecutive 16-byte units per instruction, and land where the lane that needs them
+// reads them: unit x of row r belongs to lane 4 (r % 8) + x % 4 as its unit (r / 8) U / 4 + x / 4 of U.
+template <int CH>
+struct CopyMap {
+  static constexpr int R = 32 / CH, N = kPiece / R;          // rows per instruction, instructions
+  // K: where this lane's unit of instruction n lands, less 512 (n R / 8) CH / 4 + 64 (n R % 8 rounded down to even)
+  static __device__ __forceinline__ uint32_t k_lane(int odd) {
+    const int lane = threadIdx.x & 31, x = lane % CH, lr = lane / CH + odd;
+    return (x / 4) * 512 + (((lr * 4 + x % 4) ^ ((x / 4 & 1) << 2)) * 16);
+  }
+};
+// the slot that a lane reads its K piece kc from
+__device__ __forceinline__ int k_slot(int kc) { return (threadIdx.x & 31) ^ ((kc & 1) << 2); }
+
+// Partial rows in shared memory, kRows x kWidth floats, each pair of rows turned by eight channels against the one before (so that
+// the rows of a lane quad fall into different banks).
+template <typename W>
+struct Partial {
+  static constexpr int kBytes = W::kRows * W::kWidth * 4;
+  static __device__ __forceinline__ int at(int r, int d) { return r * W::kWidth + ((d + (r >> 1 & 3) * 8) & (W::kWidth - 1)); }
+};
+
 // ---- bf16 ---------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+
 // DC: channels in units of 64; NH: query heads in units of 8
 template <int DC, int NH>
 struct WarpBf16 {
-  static constexpr int kRows = 8 * NH, kWidth = 64 * DC, KC = 2 * DC;
-  static constexpr int kStage = kPiece * kWidth * 2 * 2;     // bytes: K and V
-  uint32_t q[NH][KC][4];
-  float o[NH][4 * DC][4];
-  float m[NH][2], l[NH][2];            // heads 2 (lane % 4) and the next: reference exponent; this lane's part of the sum
+  static constexpr int kRows = 8 * NH, kWidth = 64 * DC, KC = 4 * DC;        // KC: steps of 16 channels
+  static constexpr int kRowBytes = kWidth * 2, kHalf = kPiece * kRowBytes;
+  static constexpr int kStage = 2 * kHalf;                   // bytes: K, then V
+  uint32_t q[NH][KC][2];
+  float o[NH][KC][4];                  // channels 16 t + g (and + 8), heads 2c, 2c + 1 of lane 4 g + c
+  float m[NH][2], l[NH][2];            // heads 2c and 2c + 1: reference exponent; this lane's part of the sum
 
-  __device__ __forceinline__ void load_q(const DecodeArgs& a, const char* rows, int n_rows) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  // the query rows as 16-byte units, permuted as the stages' are
+  static __device__ __forceinline__ uint32_t q_unit(int r, int x) { return r * kRowBytes + ((x ^ (r & 7)) << 4); }
+  __device__ __forceinline__ void load_q(const unsigned char* rows) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int h = 0; h < NH; ++h)
+    for (int h = 0; h < NH; ++h) {
+      // matrices of 8 heads x 8 channels: channels 0, 8, 16, 24 of two steps
+      const uint32_t at = smem_u32(rows) + (h * 8 + (lane & 7)) * kRowBytes + (((lane >> 3) ^ (lane & 7)) << 4);
 #pragma unroll
-      for (int kc = 0; kc < KC; ++kc) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (h * 8 + g < n_rows && kc * 32 + c * 8 < a.dh)
-          v = *reinterpret_cast<const uint4*>(rows + (h * 8 + g) * a.q_head + kc * 64 + c * 16);
-        q[h][kc][0] = v.x; q[h][kc][1] = v.y; q[h][kc][2] = v.z; q[h][kc][3] = v.w;
+      for (int kc = 0; kc < KC; kc += 2) {
+        uint32_t f[4];
+        ldmatrix4(f, (at ^ (kc % 4 << 5)) + kc / 4 * 128);
+        q[h][kc][0] = f[0]; q[h][kc][1] = f[1]; q[h][kc + 1][0] = f[2]; q[h][kc + 1][1] = f[3];
       }
+    }
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
 #pragma unroll
-      for (int t = 0; t < 4 * DC; ++t)
+      for (int t = 0; t < KC; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[h][t][i] = 0.f;
       m[h][0] = m[h][1] = -INFINITY;
       l[h][0] = l[h][1] = 0.f;
     }
   }
-  // copy half `half` of the tile in hand into the stage at `stage`
-  __device__ __forceinline__ void fetch(const DecodeArgs& a, const Walk& w, int tile, int half, uint32_t stage) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const uint32_t dst = stage + lane * 16;
-    // the token's own rows, if this half holds them
-    const int own = w.k_new ? w.n - 1 - tile * kTile : -1;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int j = half * kPiece + i * 8 + g;
-      const int64_t off = __shfl_sync(0xffffffffu, w.off, j);
-      const char* src = j == own ? w.k_new : w.k + off;
-      const bool ok = (w.mask >> j) & 1;
-#pragma unroll
-      for (int kc = 0; kc < KC; ++kc)
-        copy16(dst + (i * KC + kc) * 512, src + kc * 64 + c * 16, ok && kc * 32 + c * 8 < a.dh ? 16 : 0);
+  // Copy the piece in hand into the stage at `stage`: unit x of row r to r * kRowBytes + 16 (x ^ r % 8).
+  __device__ __forceinline__ void fetch(const DecodeArgs& a, const Walk& w, uint32_t stage) {
+    constexpr int CH = kWidth / 8, R = 32 / CH, N = kPiece / R;              // units of a row; rows an instruction, instructions
+    const int lane = threadIdx.x & 31, x = lane % CH, lr = lane / CH;
+    const uint32_t dst = stage + lr * kRowBytes + ((x ^ lr) << 4);           // ^ ((n R) % 8 << 4), + n R kRowBytes
+    if (a.aligned && w.mask == 0xffffu && w.own < 0 && a.dh == kWidth) {
+      const int64_t off = w.off + x * 16 + bytes_of(lr, a.row);
+      const char *k = w.k + off, *v = w.v + off;
+      if (a.row == kRowBytes / 16) {
+        unrolled<N>([&](auto cn) {
+          constexpr int r0 = decltype(cn)::value * R;
+          copy16<r0 * kRowBytes, r0 * kRowBytes>(dst ^ (r0 % 8 << 4), k, 16);
+          copy16<r0 * kRowBytes + kHalf, r0 * kRowBytes>(dst ^ (r0 % 8 << 4), v, 16);
+        });
+      } else {
+        unrolled<N>([&](auto cn) {
+          constexpr int r0 = decltype(cn)::value * R;
+          copy16<r0 * kRowBytes, 0>(dst ^ (r0 % 8 << 4), k, 16);
+          copy16<r0 * kRowBytes + kHalf, 0>(dst ^ (r0 % 8 << 4), v, 16);
+          k += bytes_of(R, a.row);
+          v += bytes_of(R, a.row);
+        });
+      }
+      return;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int j = half * kPiece + 2 * c + (i & 1) + (i >> 1) * 8;
-      const int64_t off = __shfl_sync(0xffffffffu, w.off, j);
-      const char* src = j == own ? w.v_new : w.v + off;
-      const bool ok = (w.mask >> j) & 1;
-#pragma unroll
-      for (int ch = 0; ch < DC; ++ch)
-        copy16(dst + (2 * KC + i * DC + ch) * 512, src + ch * 128 + g * 16, ok && ch * 64 + g * 8 < a.dh ? 16 : 0);
-    }
+    const bool there = x * 8 < a.dh;
+    unrolled<N>([&](auto cn) {
+      constexpr int r0 = decltype(cn)::value * R;
+      const int j = r0 + lr;
+      const int64_t off = a.aligned ? w.off + bytes_of(j, a.row) : __shfl_sync(0xffffffffu, w.off, j);
+      const int bytes = there && ((w.mask >> j) & 1) ? 16 : 0;
+      copy16<r0 * kRowBytes, 0>(dst ^ (r0 % 8 << 4), (j == w.own ? w.k_new : w.k + off) + x * 16, bytes);
+      copy16<r0 * kRowBytes + kHalf, 0>(dst ^ (r0 % 8 << 4), (j == w.own ? w.v_new : w.v + off) + x * 16, bytes);
+    });
   }
   // 16 keys; bit i of `mask`: key i counts
-  __device__ __forceinline__ void use(const DecodeArgs& a, uint32_t stage, unsigned mask) {
+  __device__ __forceinline__ void use(const DecodeArgs& a, const unsigned char* stage, unsigned mask) {
     const int lane = threadIdx.x & 31, g = lane >> 2;
-    const uint32_t src = stage + lane * 16;
-    float s[NH][4];
+    const uint32_t at = smem_u32(stage);
+    // K: matrices of 8 keys x 8 channels in the order (keys, channels) (0, 0), (8, 0), (0, 8), (8, 8)
+    const uint32_t ka = at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) << 4);
+    float s[NH][4], s2[NH][4];         // two chains of products
 #pragma unroll
     for (int h = 0; h < NH; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[h][i] = 0.f;
+      for (int i = 0; i < 4; ++i) s[h][i] = s2[h][i] = 0.f;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const uint4 lo = lds16(src + kc * 512), hi = lds16(src + (KC + kc) * 512);
+      uint32_t f[4];
+      ldmatrix4(f, (ka ^ (kc % 4 << 5)) + kc / 4 * 128);
 #pragma unroll
-      for (int h = 0; h < NH; ++h) {
-        mma16816(s[h], lo.x, hi.x, lo.y, hi.y, q[h][kc][0], q[h][kc][1]);
-        mma16816(s[h], lo.z, hi.z, lo.w, hi.w, q[h][kc][2], q[h][kc][3]);
-      }
+      for (int h = 0; h < NH; ++h) mma16816(kc & 1 ? s2[h] : s[h], f[0], f[1], f[2], f[3], q[h][kc][0], q[h][kc][1]);
     }
     // s[h][0], s[h][1]: key g, heads 2c and 2c + 1; s[h][2], s[h][3]: key g + 8
     bool grows = false;
@@ -189,7 +282,7 @@ struct WarpBf16 {
     for (int h = 0; h < NH; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[h][i] *= a.scale_log2;
+        s[h][i] = (s[h][i] + s2[h][i]) * a.scale_log2;
         if (mask != 0xffffu && !((mask >> (g + (i >> 1) * 8)) & 1)) s[h][i] = -INFINITY;
         grows |= s[h][i] > m[h][i & 1] + 8.f;
       }
@@ -207,7 +300,7 @@ struct WarpBf16 {
           m[h][e] = top;
           l[h][e] *= f;
 #pragma unroll
-          for (int t = 0; t < 4 * DC; ++t) { o[h][t][e] *= f; o[h][t][2 + e] *= f; }
+          for (int t = 0; t < KC; ++t) { o[h][t][e] *= f; o[h][t][2 + e] *= f; }
         }
     }
     uint32_t hi[NH][2], lo[NH][2];     // P^T as operand: keys 2c, 2c + 1 (and + 8) of head g
@@ -225,25 +318,20 @@ struct WarpBf16 {
         lo[h][i] = transpose8x8(pack_bf16(p[2 * i] - __uint_as_float(top << 16), p[2 * i + 1] - __uint_as_float(top & 0xffff0000u)));
       }
     }
+    // V transposed: (channels, keys) (0, 0), (8, 0), (0, 8), (8, 8)
+    const uint32_t va = at + kHalf + ((lane & 7) + (lane >> 4 << 3)) * kRowBytes + (((lane >> 3 & 1) ^ (lane & 7)) << 4);
 #pragma unroll
-    for (int ch = 0; ch < DC; ++ch) {
-      uint4 v[4];
+    for (int t = 0; t < KC; ++t) {
+      uint32_t f[4];
+      ldmatrix4_trans(f, (va ^ (t % 4 << 5)) + t / 4 * 128);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = lds16(src + (2 * KC + i * DC + ch) * 512);
+      for (int h = 0; h < NH; ++h) mma16816(o[h][t], f[0], f[1], f[2], f[3], hi[h][0], hi[h][1]);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const uint32_t a0 = __byte_perm(word(v[0], t), word(v[1], t), 0x5410), a1 = __byte_perm(word(v[0], t), word(v[1], t), 0x7632);
-        const uint32_t a2 = __byte_perm(word(v[2], t), word(v[3], t), 0x5410), a3 = __byte_perm(word(v[2], t), word(v[3], t), 0x7632);
-#pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          mma16816(o[h][ch * 4 + t], a0, a1, a2, a3, hi[h][0], hi[h][1]);
-          mma16816(o[h][ch * 4 + t], a0, a1, a2, a3, lo[h][0], lo[h][1]);
-        }
-      }
+      for (int h = 0; h < NH; ++h) mma16816(o[h][t], f[0], f[1], f[2], f[3], lo[h][0], lo[h][1]);
     }
   }
   // rows, references and sums to shared memory: o[row][channel], then m[row], l[row]
-  __device__ __forceinline__ void put(float* rows, float* ms, float* ls, int stride) {
+  __device__ __forceinline__ void put(float* rows, float* ms, float* ls) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
 #pragma unroll
     for (int h = 0; h < NH; ++h)
@@ -254,12 +342,10 @@ struct WarpBf16 {
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (g == 0) { ms[r] = m[h][e]; ls[r] = sum; }
-        // channels ch * 64 + g * 8 + 2 t + {0, 1}
 #pragma unroll
-        for (int ch = 0; ch < DC; ++ch) {
-          float4* d = reinterpret_cast<float4*>(rows + r * stride + ch * 64 + g * 8);
-          d[0] = make_float4(o[h][ch * 4][e], o[h][ch * 4][2 + e], o[h][ch * 4 + 1][e], o[h][ch * 4 + 1][2 + e]);
-          d[1] = make_float4(o[h][ch * 4 + 2][e], o[h][ch * 4 + 2][2 + e], o[h][ch * 4 + 3][e], o[h][ch * 4 + 3][2 + e]);
+        for (int t = 0; t < KC; ++t) {
+          rows[Partial<WarpBf16>::at(r, t * 16 + g)] = o[h][t][e];
+          rows[Partial<WarpBf16>::at(r, t * 16 + 8 + g)] = o[h][t][2 + e];
         }
       }
   }
@@ -277,12 +363,13 @@ struct WarpFp32 {
   static constexpr int kRows = R, kWidth = 128 * DC, KC = 8 * DC;
   static constexpr int kStage = kPiece * kWidth * 4 * 2;
   static constexpr int RL = (R + 3) / 4;                     // rows whose weights a lane computes: lane % 4 + 4 i
-  const char* qrows;
+  static constexpr int kRowBytes = kWidth * 4;
+  const unsigned char* qrows;
   float4 o[R][DC];
   float m[R], l[RL];
-  int n_rows;
 
-  __device__ __forceinline__ void load_q(const DecodeArgs& a, const char* rows, int n) { qrows = rows; n_rows = n; }
+  static __device__ __forceinline__ uint32_t q_unit(int r, int x) { return r * kRowBytes + x * 16; }
+  __device__ __forceinline__ void load_q(const unsigned char* rows) { qrows = rows; }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -293,46 +380,44 @@ struct WarpFp32 {
 #pragma unroll
     for (int i = 0; i < RL; ++i) l[i] = 0.f;
   }
-  __device__ __forceinline__ void fetch(const DecodeArgs& a, const Walk& w, int tile, int half, uint32_t stage) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const uint32_t dst = stage + lane * 16;
-    const int own = w.k_new ? w.n - 1 - tile * kTile : -1;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int j = half * kPiece + i * 8 + g;
-      const int64_t off = __shfl_sync(0xffffffffu, w.off, j);
-      const char* src = j == own ? w.k_new : w.k + off;
-      const bool ok = (w.mask >> j) & 1;
-#pragma unroll
-      for (int kc = 0; kc < KC; ++kc)
-        copy16(dst + (i * KC + kc) * 512, src + kc * 64 + c * 16, ok && kc * 16 + c * 4 < a.dh ? 16 : 0);
-    }
-#pragma unroll
-    for (int i = 0; i < kPiece; ++i) {
-      const int j = half * kPiece + i;
-      const int64_t off = __shfl_sync(0xffffffffu, w.off, j);
-      const char* src = j == own ? w.v_new : w.v + off;
-      const bool ok = (w.mask >> j) & 1;
-#pragma unroll
-      for (int d = 0; d < DC; ++d)
-        copy16(dst + (2 * KC + i * DC + d) * 512, src + d * 512 + lane * 16, ok && d * 128 + lane * 4 < a.dh ? 16 : 0);
-    }
+  __device__ __forceinline__ void fetch(const DecodeArgs& a, const Walk& w, uint32_t stage) {
+    constexpr int CH = 32;                                   // units of 128 channels; wider rows: one half after the other
+    using M = CopyMap<CH>;
+    const int lane = threadIdx.x & 31;
+    const uint32_t dst = stage + lane * 16, k0 = stage + M::k_lane(0), k1 = stage + M::k_lane(1);
+    const bool full = a.dh == kWidth;
+    unrolled<kPiece>([&](auto cn) {
+      constexpr int n = decltype(cn)::value, odd = n & 1;
+      const int j = n;
+      const int64_t off = a.aligned ? w.off + bytes_of(j, a.row) : __shfl_sync(0xffffffffu, w.off, j);
+      const char* src = (j == w.own ? w.k_new : w.k + off) + lane * 16;
+      const int bytes = (w.mask >> j) & 1 ? 16 : 0;
+      unrolled<DC>([&](auto cd) {
+        constexpr int d = decltype(cd)::value;
+        copy16<((n / 8) * KC + d * 8) * 512 + (n % 8 - odd) * 64, d * 512>(odd ? k1 : k0, src, full || d * 128 + lane * 4 < a.dh ? bytes : 0);
+      });
+    });
+    unrolled<kPiece>([&](auto ci) {
+      constexpr int i = decltype(ci)::value;
+      const int j = i;
+      const int64_t off = a.aligned ? w.off + bytes_of(j, a.row) : __shfl_sync(0xffffffffu, w.off, j);
+      const char* src = (j == w.own ? w.v_new : w.v + off) + lane * 16;
+      const int bytes = (w.mask >> j) & 1 ? 16 : 0;
+      unrolled<DC>([&](auto cd) { constexpr int d = decltype(cd)::value; copy16<(2 * KC + i * DC + d) * 512, d * 512>(dst, src, full || d * 128 + lane * 4 < a.dh ? bytes : 0); });
+    });
   }
-  __device__ __forceinline__ void use(const DecodeArgs& a, uint32_t stage, unsigned mask) {
+  __device__ __forceinline__ void use(const DecodeArgs& a, const unsigned char* stage, unsigned mask) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const uint32_t src = stage + lane * 16;
+    const uint4* src = reinterpret_cast<const uint4*>(stage);
     float s[2][R];
 #pragma unroll
     for (int r = 0; r < R; ++r) s[0][r] = s[1][r] = 0.f;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const uint4 u0 = lds16(src + kc * 512), u1 = lds16(src + (KC + kc) * 512);
-      const bool there = kc * 16 + c * 4 < a.dh;
+      const uint4 u0 = src[kc * 32 + k_slot(kc)], u1 = src[(KC + kc) * 32 + k_slot(kc)];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        // (the query rows stay in L1: 16 bytes per lane quad)
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (there && r < n_rows) x = *reinterpret_cast<const float4*>(qrows + r * a.q_head + kc * 64 + c * 16);
+        const float4 x = *reinterpret_cast<const float4*>(qrows + r * kRowBytes + kc * 64 + c * 16);
         s[0][r] = fmaf(__uint_as_float(u0.x), x.x, fmaf(__uint_as_float(u0.y), x.y, fmaf(__uint_as_float(u0.z), x.z, fmaf(__uint_as_float(u0.w), x.w, s[0][r]))));
         s[1][r] = fmaf(__uint_as_float(u1.x), x.x, fmaf(__uint_as_float(u1.y), x.y, fmaf(__uint_as_float(u1.z), x.z, fmaf(__uint_as_float(u1.w), x.w, s[1][r]))));
       }
@@ -380,7 +465,7 @@ struct WarpFp32 {
     for (int i = 0; i < kPiece; ++i) {
       uint4 v[DC];
 #pragma unroll
-      for (int d = 0; d < DC; ++d) v[d] = lds16(src + (2 * KC + i * DC + d) * 512);
+      for (int d = 0; d < DC; ++d) v[d] = src[(2 * KC + i * DC + d) * 32 + lane];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const float w = __shfl_sync(0xffffffffu, p[i >> 3][r >> 2], (i & 7) * 4 + (r & 3));
@@ -394,7 +479,7 @@ struct WarpFp32 {
       }
     }
   }
-  __device__ __forceinline__ void put(float* rows, float* ms, float* ls, int stride) {
+  __device__ __forceinline__ void put(float* rows, float* ms, float* ls) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
 #pragma unroll
     for (int i = 0; i < RL; ++i) {
@@ -407,22 +492,10 @@ struct WarpFp32 {
     for (int r = 0; r < R; ++r) {
       if (lane == 0) ms[r] = m[r];
 #pragma unroll
-      for (int d = 0; d < DC; ++d) *reinterpret_cast<float4*>(rows + r * stride + d * 128 + lane * 4) = o[r][d];
+      for (int d = 0; d < DC; ++d) *reinterpret_cast<float4*>(rows + Partial<WarpFp32>::at(r, d * 128 + lane * 4)) = o[r][d];
     }
   }
   static __device__ __forceinline__ void store4(char* row, int d, const float4& v) { *reinterpret_cast<float4*>(row + d * 4) = v; }
-};
-
-// Partial rows in shared memory: kRows x (kWidth + pad) floats, references, sums.
-template <typename W>
-struct Partial {
-  static constexpr int kStride = W::kWidth + 4;
-  static constexpr int kFloats = W::kRows * (kStride + 2);
-  static constexpr int kBytes = (kFloats * 4 + 127) / 128 * 128;
-  float* base;
-  __device__ __forceinline__ float* rows() const { return base; }
-  __device__ __forceinline__ float* ms() const { return base + W::kRows * kStride; }
-  __device__ __forceinline__ float* ls() const { return base + W::kRows * (kStride + 1); }
 };
 
 __device__ __forceinline__ void axpy(float4& acc, float w, const float4& v) {
@@ -431,52 +504,59 @@ __device__ __forceinline__ void axpy(float4& acc, float w, const float4& v) {
 // weight of a part with reference m where the largest is `top`
 __device__ __forceinline__ float part_weight(float m, float top) { return top == -INFINITY ? 0.f : exp2_approx(m - top); }
 
-// A warp's share of a request: tiles first, first + step, ... of its keys.
+// A warp's ring and the pieces it walks, those of its Walk below `end`.  start() sends the first copies on their way, run()
+// uses the pieces; between the two, and behind run(), the stage at `to` is free.
 template <typename W, int NS>
-__device__ __forceinline__ void walk_tiles(const DecodeArgs& a, W& acc, Walk& w, int first, int step, int end, uint32_t ring) {
-  const int n_pieces = first < end ? 2 * ((end - first + step - 1) / step) : 0;
-  unsigned masks[NS];                  // of the stages in flight, oldest first
-#pragma unroll
-  for (int i = 0; i < NS; ++i) masks[i] = 0;
-  int tile = first, half = 0, to = 0, from = 0;
-  auto fetch = [&](int i, unsigned& mask) {
+struct Ring {
+  unsigned char* base;
+  int n_pieces, to, from;
+  unsigned masks[NS];                  // keys that count, of the stages in flight, oldest first
+
+  __device__ __forceinline__ void fetch(const DecodeArgs& a, W& acc, Walk& w, int i, unsigned& mask) {
     mask = 0;
     if (i < n_pieces) {
-      if (half == 0) {
-        w.locate(a, tile);
-        w.page_no = w.page_of(a, tile + step, w.n);
-      }
-      acc.fetch(a, w, tile, half, ring + to * W::kStage);
-      mask = (w.mask >> (half * kPiece)) & 0xffffu;
-      if (half) tile += step;
-      half ^= 1;
+      w.locate(a, i);
+      acc.fetch(a, w, smem_u32(base) + to * W::kStage);
+      mask = w.mask;
       to = to + 1 == NS ? 0 : to + 1;
     }
-    copy_commit();
-  };
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i) fetch(i, masks[i]);
-  for (int i = 0; i < n_pieces; ++i) {
-    copy_wait<NS - 2>();
-    fetch(i + NS - 1, masks[NS - 1]);
-    if (masks[0]) acc.use(a, ring + from * W::kStage, masks[0]);
-    from = from + 1 == NS ? 0 : from + 1;
-#pragma unroll
-    for (int j = 0; j < NS - 1; ++j) masks[j] = masks[j + 1];
+    tc::cp_async_commit();
   }
-  copy_wait<0>();
-  __syncwarp();                        // the ring is free for all lanes
-}
+  __device__ __forceinline__ void start(const DecodeArgs& a, W& acc, Walk& w, int end) {
+    n_pieces = w.first < end ? unsigned(end - w.first + w.step - 1) / unsigned(w.step) : 0;
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i) fetch(a, acc, w, i, masks[i]);
+  }
+  // `late` is called once, when the last copies are about to be sent
+  template <typename F>
+  __device__ __forceinline__ void run(const DecodeArgs& a, W& acc, Walk& w, F late) {
+    const int call_at = max(n_pieces - NS, 0);
+    if (n_pieces == 0) late();
+    for (int i = 0; i < n_pieces; ++i) {
+      if (i == call_at) late();
+      tc::cp_async_wait<NS - 2>();
+      __syncwarp();                    // all lanes' copies are there, and the stage before is free
+      fetch(a, acc, w, i + NS - 1, masks[NS - 1]);
+      if (masks[0]) acc.use(a, base + from * W::kStage, masks[0]);
+      from = from + 1 == NS ? 0 : from + 1;
+#pragma unroll
+      for (int j = 0; j < NS - 1; ++j) masks[j] = masks[j + 1];
+    }
+    __syncwarp();
+  }
+};
 
 // the token's own rows into the cache
 __device__ __forceinline__ void write_own(const DecodeArgs& a, const Walk& w, int bytes) {
-  const int key = w.n - 1;
-  int page = 0;
-  int64_t off = int64_t(key) * a.row;
+  const unsigned key = w.n - 1;
+  int64_t off;
   if (w.table) {
-    page = w.table[key / a.page_size];
-    off = int64_t(page) * a.page + int64_t(key % a.page_size) * a.row;
+    const unsigned block = Walk::block_of(a, key);
+    const int page = w.table[block];
     if (unsigned(page) >= unsigned(a.n_pages)) return;
+    off = bytes_of(page, a.page) + bytes_of(key - block * unsigned(a.page_size), a.row);
+  } else {
+    off = bytes_of(key, a.row);
   }
   for (int i = (threadIdx.x & 31) * 16; i < bytes; i += 512) {
     *reinterpret_cast<uint4*>(const_cast<char*>(w.k) + off + i) = *reinterpret_cast<const uint4*>(w.k_new + i);
@@ -484,156 +564,468 @@ __device__ __forceinline__ void write_own(const DecodeArgs& a, const Walk& w, in
   }
 }
 
-__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t peer_addr(uint32_t a, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  return r;
-}
-__device__ __forceinline__ float ld_peer(uint32_t a) { float v; asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a)); return v; }
-__device__ __forceinline__ float4 ld_peer4(uint32_t a) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
-  return v;
+// the query rows of a (request, head, row block) on their way to shared memory; units behind a row and rows behind the last are zero
+template <typename W, int THREADS>
+__device__ __forceinline__ void copy_q(const DecodeArgs& a, unsigned char* to, int b, int head0, int n_rows) {
+  constexpr int CH = W::kRowBytes / 16, EL = W::kRowBytes / W::kWidth;
+  const char* rows = a.q + bytes_of(b, a.q_batch) + bytes_of(head0, a.q_head);
+#pragma unroll
+  for (int u = threadIdx.x; u < W::kRows * CH; u += THREADS) {
+    const int r = u / CH, x = u % CH;
+    copy16<0, 0>(smem_u32(to) + W::q_unit(r, x), rows + (r < n_rows ? bytes_of(r, a.q_head) : 0) + x * 16, r < n_rows && x * 16 < a.dh * EL ? 16 : 0);
+  }
+  tc::cp_async_commit();
 }
 
-// One cluster per (request, key head, block of query heads): its warps take the tiles in turn; their parts meet in shared
-// memory, the CTAs' parts in distributed shared memory.
-template <typename W, int WARPS, int NS>
-__global__ void __launch_bounds__(32 * WARPS) decode_cluster_kernel(const __grid_constant__ DecodeArgs a, int cluster) {
+// where the warps of a CTA leave their partial rows (bytes into its shared memory), references and sums
+template <typename W, int WARPS>
+struct Meeting {
+  int at[WARPS];
+  float m[WARPS][W::kRows], l[WARPS][W::kRows];
+};
+// row r, channels d .. d + 3 of all warps
+template <typename W, int WARPS>
+__device__ __forceinline__ float4 join_warps(const unsigned char* smem, const Meeting<W, WARPS>& meet, int r, int d, float& top, float& sum) {
+  top = meet.m[0][r];
+  sum = 0.f;
+#pragma unroll
+  for (int i = 1; i < WARPS; ++i) top = fmaxf(top, meet.m[i][r]);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < WARPS; ++i) {
+    const float f = part_weight(meet.m[i][r], top);
+    sum = fmaf(f, meet.l[i][r], sum);
+    axpy(o, f, *reinterpret_cast<const float4*>(smem + meet.at[i] + Partial<W>::at(r, d) * 4));
+  }
+  return o;
+}
+template <typename W>
+__device__ __forceinline__ void store_row(const DecodeArgs& a, int b, int head, int d, float4 o, float top, float sum) {
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
+  W::store4(a.out + bytes_of(b, a.out_batch) + bytes_of(head, a.out_head), d, o);
+  if (d == 0 && a.lse) a.lse[b * a.lse_batch + head * a.lse_head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) / kLog2e;
+}
+__device__ __forceinline__ void report(const DecodeArgs& a, bool bad, bool cut) {
+  if (!a.status) return;
+  bad = __any_sync(0xffffffffu, bad);
+  cut = __any_sync(0xffffffffu, cut);
+  if ((threadIdx.x & 31) == 0 && (bad || cut)) atomicOr(a.status, (bad ? LIGHTKV_STATUS_PAGE : 0u) | (cut ? LIGHTKV_STATUS_COUNT : 0u));
+}
+template <typename W> __host__ __device__ constexpr int row_bytes(int dh) { return dh * (W::kRowBytes / W::kWidth); }
+template <typename W> __host__ __device__ constexpr int q_bytes() { return W::kRows * W::kRowBytes; }
+
+// room for the quads that a CTA of a cluster gets from its peers, times the cluster's size: rounds of the output, each of
+// 32 quads per CTA, rounded up
+template <typename W> __host__ __device__ constexpr int part_quads() {
+  return W::kRows * W::kWidth / 4 + 32 * kMaxCluster;
+}
+
+// One cluster per (request, key head, block of query heads): its warps take the pieces in turn; their parts meet in shared
+// memory.  Each CTA of a cluster finishes its share of the output: the others send it their parts of that.
+template <typename W, int WARPS, int NS, int PER_SM>
+__global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_cluster_kernel(const __grid_constant__ DecodeArgs a, int cluster) {
+  // the warps' rings | query rows | parts of the cluster's CTAs: rows, references, sums
   extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int THREADS = 32 * WARPS, kRings = WARPS * NS * W::kStage, QUADS = W::kWidth / 4;
+  __shared__ Meeting<W, WARPS> meet;
   grid_dependency_sync();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = cluster > 1 ? (int)cluster_rank() : 0;
-  const int unit = blockIdx.x / cluster;
-  const int rb = unit % a.row_blocks, hk = unit / a.row_blocks % a.n_kv_heads, b = unit / a.row_blocks / a.n_kv_heads;
+  const int warp = threadIdx.x >> 5;
+  const int rank = cluster > 1 ? (int)tc::cluster_ctarank() : 0;
+  const int unit = blockIdx.x / unsigned(cluster);
+  const int per_b = a.n_kv_heads * a.row_blocks, b = unit / unsigned(per_b), head = unit - b * per_b;
+  const int hk = a.row_blocks == 1 ? head : head / a.row_blocks, rb = head - hk * a.row_blocks;
   const int first = rank * WARPS + warp, step = cluster * WARPS;
   Walk w;
-  w.table = a.table ? a.table + size_t(b) * a.max_blocks : nullptr;
-  w.k = a.k + hk * a.head + (a.table ? 0 : b * a.page);
-  w.v = a.v + hk * a.head + (a.table ? 0 : b * a.page);
-  w.k_new = a.k_new ? a.k_new + b * a.new_batch + hk * a.new_head : nullptr;
-  w.v_new = a.k_new ? a.v_new + b * a.new_batch + hk * a.new_head : nullptr;
-  w.bad = false;
-  w.page_no = w.page_of(a, first, (int)min(a.cap, 0x7fffffffll));    // in flight beside the number of keys
+  w.start(a, b, hk, first, step);
+  w.look(a, a.cap);                    // in flight beside the number of keys
   const int asked = a.n_keys[b];
-  w.n = (int)min((long long)max(asked, 0), a.cap);
   const int head0 = hk * a.group + rb * W::kRows, n_rows = min(W::kRows, a.group - rb * W::kRows);
+  copy_q<W, THREADS>(a, smem + kRings, b, head0, n_rows);
+  if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // all CTAs of the cluster run
+  w.n = min(max(asked, 0), a.cap);
   W acc;
-  acc.load_q(a, a.q + b * a.q_batch + head0 * a.q_head, n_rows);
+  Ring<W, NS> ring;
+  ring.base = smem + warp * (NS * W::kStage);
+  ring.to = ring.from = 0;
+  ring.start(a, acc, w, (int)((unsigned(w.n) + kPiece - 1) / kPiece));
+  tc::cp_async_wait<NS - 1>();
+  __syncthreads();                     // the query rows are there
+  acc.load_q(smem + kRings);
   acc.clear();
-  unsigned char* ring = smem + warp * (NS * W::kStage);
-  const int n_tiles = (int)(((long long)w.n + kTile - 1) / kTile);
-  walk_tiles<W, NS>(a, acc, w, first, step, n_tiles, smem_addr(ring));
-  if (rb == 0 && w.k_new && w.n > 0 && ((w.n - 1) / kTile) % step == first) write_own(a, w, a.dh * (W::kStage / (kPiece * W::kWidth * 2)));
-  if (a.status) {
-    const bool bad = __any_sync(0xffffffffu, w.bad);
-    if (lane == 0 && (bad || (warp == 0 && asked > w.n)))
-      atomicOr(a.status, (bad ? LIGHTKV_STATUS_PAGE : 0u) | (asked > w.n ? LIGHTKV_STATUS_COUNT : 0u));
-  }
+  ring.run(a, acc, w, [] {});
+  if (rb == 0 && w.k_new && w.n > 0 && unsigned(w.n - 1) / kPiece % step == first) write_own(a, w, row_bytes<W>(a.dh));
+  report(a, w.bad, warp == 0 && asked > w.n);
 
-  using P = Partial<W>;
-  static_assert(2 * P::kBytes <= NS * W::kStage, "a warp's ring holds its partial rows and the CTA's");
-  P mine{reinterpret_cast<float*>(ring)};
-  acc.put(mine.rows(), mine.ms(), mine.ls(), P::kStride);
+  static_assert(Partial<W>::kBytes <= W::kStage, "a stage holds a warp's partial rows");
+  unsigned char* mine = ring.base + ring.to * W::kStage;
+  if ((threadIdx.x & 31) == 0) meet.at[warp] = int(mine - smem);
+  acc.put(reinterpret_cast<float*>(mine), meet.m[warp], meet.l[warp]);
+  if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   __syncthreads();
-  const int quads = a.dh / 4;
-  P cta{reinterpret_cast<float*>(smem + P::kBytes)};         // behind warp 0's part
-  auto part = [&](int i) { return P{reinterpret_cast<float*>(smem + i * (NS * W::kStage))}; };
-  for (int u = threadIdx.x; u < n_rows * quads; u += 32 * WARPS) {
-    const int r = u / quads, d = (u - r * quads) * 4;
-    float top = part(0).ms()[r], sum = 0.f;
-#pragma unroll
-    for (int i = 1; i < WARPS; ++i) top = fmaxf(top, part(i).ms()[r]);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) {
-      const float f = part_weight(part(i).ms()[r], top);
-      sum = fmaf(f, part(i).ls()[r], sum);
-      axpy(o, f, *reinterpret_cast<const float4*>(part(i).rows() + r * P::kStride + d));
-    }
+  // every 32 quads of the output are finished by another CTA, in whose shared memory lie the parts of quad u from all of them
+  const uint32_t parts = smem_u32(smem + kRings + q_bytes<W>());
+  const int n_quads = n_rows * QUADS;
+  for (int u = threadIdx.x; u < n_quads; u += THREADS) {
+    const int r = u / QUADS, d = u % QUADS * 4;
+    float top, sum;
+    const float4 o = join_warps<W, WARPS>(smem, meet, r, d, top, sum);
     if (cluster == 1) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-      W::store4(a.out + b * a.out_batch + (head0 + r) * a.out_head, d, o);
-      if (d == 0 && a.lse) a.lse[b * a.lse_batch + (head0 + r) * a.lse_head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) / kLog2e;
+      if (d < a.dh) store_row<W>(a, b, head0 + r, d, o, top, sum);
     } else {
-      *reinterpret_cast<float4*>(cta.rows() + r * P::kStride + d) = o;
-      if (d == 0) { cta.ms()[r] = top; cta.ls()[r] = sum; }
+      const int owner = u / 32 % cluster;
+      const uint32_t at = tc::map_to_cta(parts + ((u / 32 / cluster * 32 + u % 32) * cluster + rank) * 16, owner);
+      const uint32_t ml = tc::map_to_cta(parts + part_quads<W>() * 16 + (r * cluster + rank) * 8, owner);
+      asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(o.x), "f"(o.y), "f"(o.z), "f"(o.w) : "memory");
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(ml), "f"(top), "f"(sum) : "memory");
     }
   }
   if (cluster == 1) return;
   cluster_sync();
-  for (int u = rank * 32 * WARPS + threadIdx.x; u < n_rows * quads; u += cluster * 32 * WARPS) {
-    const int r = u / quads, d = (u - r * quads) * 4;
-    const uint32_t am = smem_addr(cta.ms() + r), al = smem_addr(cta.ls() + r), ao = smem_addr(cta.rows() + r * P::kStride + d);
-    float top = -INFINITY, sum = 0.f;
+  const float4* rows = reinterpret_cast<const float4*>(smem + kRings + q_bytes<W>());
+  const float2* sums = reinterpret_cast<const float2*>(rows + part_quads<W>());
+  for (int j = warp; (j * cluster + rank) * 32 < n_quads; j += WARPS) {
+    const int u = (j * cluster + rank) * 32 + threadIdx.x % 32, r = u / QUADS, d = u % QUADS * 4;
+    if (u >= n_quads) break;
+    float top = sums[r * cluster].x, sum = 0.f;
+    for (int i = 1; i < cluster; ++i) top = fmaxf(top, sums[r * cluster + i].x);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    float ms[8], ls[8];
-    float4 os[8];
-    for (int base = 0; base < cluster; base += 8) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (base + i < cluster) {
-          ms[i] = ld_peer(peer_addr(am, base + i));
-          ls[i] = ld_peer(peer_addr(al, base + i));
-          os[i] = ld_peer4(peer_addr(ao, base + i));
-        }
-      float next = top;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) if (base + i < cluster) next = fmaxf(next, ms[i]);
-      const float f = part_weight(top, next);
-      sum *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
-      top = next;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (base + i < cluster) {
-          const float g = part_weight(ms[i], top);
-          sum = fmaf(g, ls[i], sum);
-          axpy(o, g, os[i]);
-        }
+    for (int i = 0; i < cluster; ++i) {
+      const float2 ml = sums[r * cluster + i];
+      const float f = part_weight(ml.x, top);
+      sum = fmaf(f, ml.y, sum);
+      axpy(o, f, rows[(j * 32 + threadIdx.x % 32) * cluster + i]);
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-    W::store4(a.out + b * a.out_batch + (head0 + r) * a.out_head, d, o);
-    if (d == 0 && a.lse) a.lse[b * a.lse_batch + (head0 + r) * a.lse_head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) / kLog2e;
+    if (d < a.dh) store_row<W>(a, b, head0 + r, d, o, top, sum);
   }
-  cluster_sync();                      // a CTA's shared memory lives until all have read it
 }
 
-template <typename W, int WARPS, int NS>
-cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, cudaStream_t stream) {
+// ---- items ----------------------------------------------------------------------------------------------------------------
+// A request's keys are cut into equal parts of about total / MOST blocks of kPiece keys per warp (MOST: kItemsPerSlot for each CTA
+// that fits on the SMs), one item per part, key head and row block.  CTAs take items as they become free: a resident CTA cancels
+// the launch of one that has not started and does its work.  (Fixed equal shares of all keys, cut wherever they end, 132 against
+// 95 us for 96 requests of 37 to 8192 keys: shares of many short requests take longer.)  The parts of a request that was cut go to
+// the workspace and are joined by decode_join_kernel.
+struct JoinRecord { int b, head0, parts, slot; };
+struct JoinHeader { int n; int pad[63]; };
+constexpr int kItemsPerSlot = 2;
+constexpr int kMinBlocks = 4;         // of a part
+
+template <typename W> __host__ __device__ constexpr int part_floats() { return (W::kRows * (W::kWidth + 2) + 3) / 4 * 4; }   // rows on 16 bytes
+// With n blocks in all and parts of c >= n / most, fewer than `most` requests are cut (heads and row blocks counted apart), into fewer
+// than 2 `most` parts, and there are fewer than `most` items more than requests.
+template <typename W> constexpr size_t items_bytes(int most) {
+  return sizeof(JoinHeader) + (size_t(most) * sizeof(JoinRecord) + 255) / 256 * 256 + size_t(most) * 2 * part_floats<W>() * 4;
+}
+
+template <typename W, int WARPS, int NS, int PER_SM, int MOST>
+__global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const __grid_constant__ DecodeArgs a, int batch, JoinHeader* header,
+                                                                         JoinRecord* records, float* parts) {
+  // the warps' rings | query rows of this item and the next
+  extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int THREADS = 32 * WARPS, kBlock = kPiece * WARPS, kRings = WARPS * NS * W::kStage, QUADS = W::kWidth / 4;
+  __shared__ unsigned warp_blocks[WARPS];
+  __shared__ int warp_sums[3][WARPS];
+  __shared__ int items_at[THREADS + 1], slots_at[THREADS], splits_at[THREADS], keys_at[THREADS];   // per run of requests
+  __shared__ Meeting<W, WARPS> meet;
+  __shared__ __align__(16) unsigned char answer[16];
+  __shared__ __align__(8) uint64_t answered;
+  __shared__ int abort_flag;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  if (t == 0) {
+    tc::mbar_init(&answered, 1);
+    tc::fence_barrier_init();
+    abort_flag = 0;
+  }
+  grid_dependency_sync();
+  const int heads = a.n_kv_heads * a.row_blocks;
+  auto keys_of = [&](int b) { return min(max(a.n_keys[b], 0), a.cap); };
+  auto blocks_of = [&](int n) { return (unsigned(n) + kBlock - 1) / kBlock; };
+
+  // all blocks (the host has seen to it that they are counted in 32 bits); each thread looks at a run of requests
+  const int run = unsigned(batch + THREADS - 1) / THREADS, b_lo = min(t * run, batch), b_hi = min(b_lo + run, batch);
+  unsigned blocks = 0;
+  int n0 = 0;
+  for (int b = b_lo; b < b_hi; ++b) blocks += blocks_of(n0 = keys_of(b));
+  keys_at[t] = n0;                     // of use where a run is one request
+  {
+    // sums of 16 bits each, so that a warp's fit 32
+    const unsigned lo = __reduce_add_sync(0xffffffffu, blocks & 0xffffu), hi = __reduce_add_sync(0xffffffffu, blocks >> 16);
+    if (lane == 0) warp_blocks[warp] = (hi << 16) + lo;
+  }
+  __syncthreads();
+  unsigned total = 0;
+#pragma unroll
+  for (int i = 0; i < WARPS; ++i) total += warp_blocks[i];
+  const unsigned chunk = max(unsigned(kMinBlocks), unsigned(((unsigned long long)total * heads + MOST - 1) / MOST));
+  auto parts_of = [&](int n) { return n > 0 ? (blocks_of(n) + chunk - 1) / chunk : 1u; };
+  // items, slots of cut requests and cut requests in front of the run
+  int sums[3] = {0, 0, 0};
+  for (int b = b_lo; b < b_hi; ++b) {
+    const int p = parts_of(run == 1 ? n0 : keys_of(b));
+    sums[0] += p * heads;
+    if (p > 1) { sums[1] += p * heads; sums[2] += heads; }
+  }
+  int upto[3] = {sums[0], sums[1], sums[2]};
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int o = __shfl_up_sync(0xffffffffu, upto[i], d);
+      if (lane >= d) upto[i] += o;
+    }
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (lane == 31) warp_sums[i][warp] = upto[i];
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < WARPS; ++j)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) upto[i] += j < warp ? warp_sums[i][j] : 0;
+  items_at[t + 1] = upto[0];
+  if (t == 0) items_at[0] = 0;
+  slots_at[t] = upto[1] - sums[1];
+  splits_at[t] = upto[2] - sums[2];
+  if (blockIdx.x == 0 && t == THREADS - 1) header->n = upto[2];
+  __syncthreads();
+  const int n_items = items_at[THREADS];
+  if (int(blockIdx.x) >= n_items) return;
+
+  struct Item { int b, n, parts, part, slot, record, head0, n_rows; };
+  static_assert(Partial<W>::kBytes <= W::kStage, "a stage holds a warp's partial rows");
+  bool bad = false, cut = false;
+  uint32_t parity = 0;
+  Walk w;
+  W acc;
+  Ring<W, NS> ring;
+  ring.base = smem + warp * (NS * W::kStage);
+  ring.to = ring.from = 0;
+  Item it = {};
+  int item = blockIdx.x;
+  for (int q_at = 0;; q_at ^= 1) {     // (the first time round nothing is under way yet)
+    const Item now = it;
+    const bool open = now.parts > 0;
+    bool heard = true;
+    if (open) {
+      acc.load_q(smem + kRings + (q_at ^ 1) * q_bytes<W>());
+      acc.clear();
+      ring.run(a, acc, w, [&] {        // which item comes next: asked late, so that no CTA sits on one that others could start
+        if (t == 0) {
+          tc::mbar_expect_tx(&answered, 16);
+          tc::clc_try_cancel(answer, &answered);
+        }
+      });
+      bad |= w.bad;
+      heard = tc::mbar_wait(&answered, parity, &abort_flag);
+      parity ^= 1;
+      item = heard ? tc::clc_canceled_cta(answer) : -1;
+      tc::fence_proxy_async();         // the answer has been read before the next one is written
+      if (!heard && a.status) atomicOr(a.status, LIGHTKV_STATUS_TIMEOUT);
+    }
+    // the next item's copies are sent on their way before the parts of this one meet
+    const bool more = item >= 0 && item < n_items;
+    if (more) {
+      int r = 0;
+#pragma unroll
+      for (int d = THREADS / 2; d; d >>= 1)
+        if (items_at[r + d] <= item) r += d;
+      it.b = r * run; it.n = run == 1 ? keys_at[r] : keys_of(it.b); it.parts = parts_of(it.n);
+      int i = item - items_at[r];
+      it.slot = slots_at[r]; it.record = splits_at[r];
+      while (i >= it.parts * heads) {  // (runs of several requests)
+        i -= it.parts * heads;
+        if (it.parts > 1) { it.slot += it.parts * heads; it.record += heads; }
+        it.n = keys_of(++it.b);
+        it.parts = parts_of(it.n);
+      }
+      const int head = it.parts == 1 ? i : unsigned(i) / unsigned(it.parts);
+      it.part = i - head * it.parts;
+      it.slot += i;
+      it.record += head;
+      const int hk = a.row_blocks == 1 ? head : head / a.row_blocks, rb = head - hk * a.row_blocks;
+      it.head0 = hk * a.group + rb * W::kRows;
+      it.n_rows = min(W::kRows, a.group - rb * W::kRows);
+      const int per = it.parts == 1 ? blocks_of(it.n) : (blocks_of(it.n) + it.parts - 1) / unsigned(it.parts);
+      const int first = it.part * per * WARPS + warp, end = min((it.part + 1) * per * WARPS, int((unsigned(it.n) + kPiece - 1) / kPiece));
+      w.start(a, it.b, hk, first, WARPS);
+      w.n = it.n;
+      w.look(a, it.n);
+      copy_q<W, THREADS>(a, smem + kRings + q_at * q_bytes<W>(), it.b, it.head0, it.n_rows);
+      cut |= it.n == a.cap && a.n_keys[it.b] > it.n;
+      const int last = (it.n - 1) / kPiece;
+      if (rb == 0 && w.k_new && it.n > 0 && last >= first && last < end && unsigned(last - first) % WARPS == 0) write_own(a, w, row_bytes<W>(a.dh));
+      ring.start(a, acc, w, end);
+    }
+    if (open) {
+      unsigned char* own = ring.base + ring.to * W::kStage;
+      if (lane == 0) meet.at[warp] = int(own - smem);
+      acc.put(reinterpret_cast<float*>(own), meet.m[warp], meet.l[warp]);
+      __syncthreads();
+      float* mine = parts + size_t(now.slot) * part_floats<W>();
+      for (int u = t; u < now.n_rows * QUADS; u += THREADS) {
+        const int row = u / QUADS, d = u % QUADS * 4;
+        float top, sum;
+        const float4 o = join_warps<W, WARPS>(smem, meet, row, d, top, sum);
+        if (now.parts == 1) {
+          if (d < a.dh) store_row<W>(a, now.b, now.head0 + row, d, o, top, sum);
+        } else {
+          *reinterpret_cast<float4*>(mine + row * W::kWidth + d) = o;
+          if (d == 0) { mine[W::kRows * W::kWidth + row] = top; mine[W::kRows * (W::kWidth + 1) + row] = sum; }
+        }
+      }
+      if (t == 0 && now.parts > 1 && now.part == 0) records[now.record] = {now.b, now.head0, now.parts, now.slot};
+    }
+    if (more) tc::cp_async_wait<NS - 1>();                   // the query rows are there
+    if (__syncthreads_or(!heard) || !more) break;
+  }
+  tc::cp_async_wait<0>();
+  report(a, bad, cut);
+}
+
+// The parts of a request that was cut: CTAs take one record after the other and `rows` rows of it; groups of threads take the parts
+// in turn.
+template <typename W>
+__global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs a, int rows, const JoinHeader* header,
+                                                          const JoinRecord* records, const float* parts) {
+  __shared__ float4 os[256];
+  __shared__ float tops[256], sums[256];
+  constexpr int QUADS = W::kWidth / 4;
+  grid_dependency_sync();
+  const int n = header->n;
+  JoinRecord rec = records[blockIdx.x];                      // (beside the number; behind it: anything)
+  for (int i_rec = blockIdx.x; i_rec < n; i_rec += gridDim.x) {
+    if (i_rec != int(blockIdx.x)) rec = records[i_rec];
+    const int r0 = blockIdx.y * rows, outputs = min(rows, min(W::kRows, a.group - rec.head0 % a.group) - r0) * QUADS;
+    const int per_round = min(outputs, 256), groups = outputs > 0 ? 256 / per_round : 0, g = outputs > 0 ? threadIdx.x / per_round : 0;
+    const int used = min(groups, rec.parts);
+    const float* first = parts + size_t(rec.slot) * part_floats<W>();
+    for (int base = 0; base < outputs; base += per_round) {
+      const int u = base + threadIdx.x - g * per_round, r = r0 + u / QUADS, d = u % QUADS * 4;
+      const bool mine = g < used && u < outputs;
+      float top = -INFINITY, sum = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      constexpr int J = 6;
+      if (mine)
+        for (int i0 = g; i0 < rec.parts; i0 += J * groups) {
+          float m[J], l[J];
+          float4 x[J];
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            const int i = i0 + j * groups;
+            m[j] = -INFINITY; l[j] = 0.f; x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i < rec.parts) {
+              const float* p = first + size_t(i) * part_floats<W>();
+              m[j] = p[W::kRows * W::kWidth + r]; l[j] = p[W::kRows * (W::kWidth + 1) + r];
+              x[j] = *reinterpret_cast<const float4*>(p + r * W::kWidth + d);
+            }
+          }
+          float next = top;
+#pragma unroll
+          for (int j = 0; j < J; ++j) next = fmaxf(next, m[j]);
+          const float f = part_weight(top, next);
+          sum *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+          top = next;
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            const float e = part_weight(m[j], top);
+            sum = fmaf(e, l[j], sum);
+            axpy(o, e, x[j]);
+          }
+        }
+      if (used > 1) {
+        os[threadIdx.x] = o; tops[threadIdx.x] = top; sums[threadIdx.x] = sum;
+        __syncthreads();
+        if (g == 0) {
+          const float own = top;
+          for (int i = 1; i < used; ++i) top = fmaxf(top, tops[i * per_round + threadIdx.x]);
+          const float f = part_weight(own, top);
+          sum *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+          for (int i = 1; i < used; ++i) {
+            const int at = i * per_round + threadIdx.x;
+            const float e = part_weight(tops[at], top);
+            sum = fmaf(e, sums[at], sum);
+            axpy(o, e, os[at]);
+          }
+        }
+        __syncthreads();
+      }
+      if (mine && g == 0 && d < a.dh) store_row<W>(a, rec.b, rec.head0 + r, d, o, top, sum);
+    }
+  }
+}
+
+// Shapes of the kernels: warps a CTA, stages of a warp's ring, CTAs per SM that fit.
+template <typename W, int WARPS> struct Shape {
+  static constexpr int kWarps = WARPS, kStages = W::kStage <= 4096 ? 6 : 3;
+  static constexpr int kRings = kWarps * kStages * W::kStage;
+  static constexpr int kPerSm = std::max(1, 227 * 1024 / (kRings + 2 * q_bytes<W>() + 5120));
+  static constexpr int kItemsSmem = kRings + 2 * q_bytes<W>();
+  static constexpr int kMost = kItemsPerSlot * kPerSm * kSms;
+};
+template <typename W> using Items = Shape<W, W::kStage <= 16384 ? 4 : 2>;
+
+template <typename W, int WARPS>
+cudaError_t launch_clusters(const DecodeArgs& a, long long units, int cluster, cudaStream_t stream) {
+  using S = Shape<W, WARPS>;
+  auto kernel = decode_cluster_kernel<W, WARPS, S::kStages, S::kPerSm>;
+  const int smem = S::kRings + q_bytes<W>() + (cluster > 1 ? part_quads<W>() * 16 + W::kRows * kMaxCluster * 8 : 0);
+  const cudaError_t e = ensure_dynamic_smem(kernel, smem);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(kernel, dim3((unsigned)(units * cluster)), dim3(32 * WARPS), smem, stream, cluster, a, cluster);
+}
+
+// Which form a call takes.  Clusters where the longest request that the caller has announced gives a warp at most kLongest pieces: CTAs
+// of eight warps, as many to a request and head as there are SMs for, up to four waves of CTAs; CTAs of four, two on an SM, for more.
+// Items behind that: their plan and the join of their parts take about 6 us, but long requests are spread over all SMs.
+//   us a call, bf16, head size 128 (64)       8 warps      4 warps      items
+//   1 x 404 keys, 32 heads                     5.2          6.2          9.4
+//   16 x 150 .. 1500, 8 key heads             13.4         14.3         18.9
+//   24 x 90 .. 2000, 8 key heads (64)         12.9         15.1         17.6
+//   48 x 301 .. 1399, 40 key heads             122          109          111
+//   96 x 0 .. 8192, 8 key heads                 99          113           94
+//   2 x 60000 .. 131072, 4 key heads           148          134           75
+constexpr int kLongest = 32;
+
+template <typename W>
+cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, cudaStream_t stream) {
+  using S = Items<W>;
   a.row_blocks = (a.group + W::kRows - 1) / W::kRows;
   const long long units = (long long)batch * a.n_kv_heads * a.row_blocks;
+  constexpr bool can_wide = W::kStage <= 8192;               // rings of eight warps fit an SM
+  const bool wide = can_wide && units <= 4 * sm_count();
+  const int warps = wide ? 8 : S::kWarps, room = wide ? sm_count() : S::kPerSm * sm_count();
   int cluster = 1;
-  while (cluster < 8 && units * cluster * 2 <= 2 * sm_count() && cluster * WARPS * kTile < max_keys) cluster *= 2;
-  constexpr size_t smem = size_t(WARPS) * NS * W::kStage;
-  const cudaError_t e = ensure_dynamic_smem(decode_cluster_kernel<W, WARPS, NS>, (int)smem);
-  if (e != cudaSuccess) return e;
-  return launch_kernel(decode_cluster_kernel<W, WARPS, NS>, dim3((unsigned)(units * cluster)), dim3(32 * WARPS), smem, stream, cluster, a, cluster);
+  while (cluster < kMaxCluster && units * cluster * 2 <= room && cluster * warps * kPiece < max_keys) cluster *= 2;
+  if ((long long)max_keys <= (long long)cluster * warps * kPiece * kLongest) {
+    if constexpr (can_wide)
+      if (wide) return launch_clusters<W, 8>(a, units, cluster, stream);
+    return launch_clusters<W, S::kWarps>(a, units, cluster, stream);
+  }
+  const int rows = std::min(a.group, W::kRows);
+  JoinHeader* header = static_cast<JoinHeader*>(workspace);
+  JoinRecord* records = reinterpret_cast<JoinRecord*>(header + 1);
+  float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + sizeof(JoinHeader) + (size_t(S::kMost) * sizeof(JoinRecord) + 255) / 256 * 256);
+  auto kernel = decode_items_kernel<W, S::kWarps, S::kStages, S::kPerSm, S::kMost>;
+  cudaError_t e = ensure_dynamic_smem(kernel, S::kItemsSmem);
+  if (e == cudaSuccess)
+    e = launch_kernel(kernel, dim3((unsigned)(units + S::kMost)), dim3(32 * S::kWarps), S::kItemsSmem, stream, 1, a, batch, header, records, parts);
+  // few requests have many parts each: a CTA joins one row of them
+  const int per_cta = units <= 64 ? 1 : rows;
+  if (e == cudaSuccess)
+    e = launch_kernel(decode_join_kernel<W>, dim3((unsigned)std::min<long long>(units, 2 * kSms), (rows + per_cta - 1) / per_cta), dim3(256), 0, stream, 1,
+                      a, per_cta, header, records, parts);
+  return e;
 }
 
-cudaError_t launch_decode(const DecodeArgs& a, int dtype, int batch, int max_keys, cudaStream_t stream) {
+// f(kernel variant) for a type, group and head size
+template <typename F>
+auto with_variant(int dtype, int group, int dh, F f) {
   if (dtype == LIGHTKV_BF16) {
-    if (a.group <= 8) {
-      if (a.dh <= 64) return launch_form<WarpBf16<1, 1>, 4, 6>(a, batch, max_keys, stream);
-      if (a.dh <= 128) return launch_form<WarpBf16<2, 1>, 4, 3>(a, batch, max_keys, stream);
-      return launch_form<WarpBf16<4, 1>, 4, 3>(a, batch, max_keys, stream);
-    }
-    if (a.dh <= 64) return launch_form<WarpBf16<1, 2>, 4, 6>(a, batch, max_keys, stream);
-    if (a.dh <= 128) return launch_form<WarpBf16<2, 2>, 4, 3>(a, batch, max_keys, stream);
-    return launch_form<WarpBf16<4, 2>, 4, 3>(a, batch, max_keys, stream);
+    if (group <= 8) return dh <= 64 ? f(WarpBf16<1, 1>()) : dh <= 128 ? f(WarpBf16<2, 1>()) : f(WarpBf16<4, 1>());
+    return dh <= 64 ? f(WarpBf16<1, 2>()) : dh <= 128 ? f(WarpBf16<2, 2>()) : f(WarpBf16<4, 2>());
   }
-  if (a.dh <= 128) {
-    if (a.group == 1) return launch_form<WarpFp32<1, 1>, 4, 3>(a, batch, max_keys, stream);
-    if (a.group <= 4) return launch_form<WarpFp32<1, 4>, 4, 3>(a, batch, max_keys, stream);
-    return launch_form<WarpFp32<1, 8>, 4, 3>(a, batch, max_keys, stream);
-  }
-  if (a.group == 1) return launch_form<WarpFp32<2, 1>, 2, 3>(a, batch, max_keys, stream);
-  return launch_form<WarpFp32<2, 4>, 2, 3>(a, batch, max_keys, stream);
+  if (dh <= 128) return group == 1 ? f(WarpFp32<1, 1>()) : group <= 4 ? f(WarpFp32<1, 4>()) : f(WarpFp32<1, 8>());
+  return group == 1 ? f(WarpFp32<2, 1>()) : f(WarpFp32<2, 4>());
 }
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -650,7 +1042,10 @@ size_t lightkv_decode_workspace(int32_t batch, int32_t n_q_heads, int32_t n_kv_h
   if (batch <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || head_dim <= 0 || head_dim % 8 || head_dim > 256 ||
       (dtype != LIGHTKV_BF16 && dtype != LIGHTKV_FP32))
     return 0;
-  return 256;
+  return with_variant(dtype, n_q_heads / n_kv_heads, head_dim, [](auto v) {
+    using W = decltype(v);
+    return items_bytes<W>(Items<W>::kMost);
+  });
 }
 
 int lightkv_decode_attention(const lightkv_decode_args_t* a) {
@@ -669,7 +1064,10 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   const int64_t el = a->dtype == LIGHTKV_BF16 ? 2 : 4;
   const int64_t strides[9] = {a->q_batch_stride, a->q_head_stride, a->page_stride, a->head_stride, a->row_stride,
                               a->new_batch_stride, a->new_head_stride, a->out_batch_stride, a->out_head_stride};
-  for (int64_t s : strides) if (s * el % 16) return LIGHTKV_ERR_INVALID_ARG;
+  for (int64_t s : strides) {
+    if (s < 0 || s * el % 16) return LIGHTKV_ERR_INVALID_ARG;
+    if (s * el / 16 > 0xffffffffll) return LIGHTKV_ERR_UNSUPPORTED;                          // strides of 64 GB and more
+  }
   if (a->row_stride < a->head_dim || a->q == a->out) return LIGHTKV_ERR_INVALID_ARG;
   if (!aligned(a->workspace, 256) ||
       a->workspace_bytes < lightkv_decode_workspace(a->batch, a->n_q_heads, a->n_kv_heads, a->head_dim, a->dtype))
@@ -682,21 +1080,31 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   d.out = static_cast<char*>(a->out);
   d.lse = a->lse; d.n_keys = a->n_keys; d.status = a->status;
   d.table = a->page_size > 0 ? a->block_table : nullptr;
-  d.q_batch = a->q_batch_stride * el; d.q_head = a->q_head_stride * el;
-  d.page = a->page_stride * el; d.head = a->head_stride * el; d.row = a->row_stride * el;
-  d.new_batch = a->new_batch_stride * el; d.new_head = a->new_head_stride * el;
-  d.out_batch = a->out_batch_stride * el; d.out_head = a->out_head_stride * el;
+  auto units = [&](int64_t stride) { return (uint32_t)(stride * el / 16); };
+  d.q_batch = units(a->q_batch_stride); d.q_head = units(a->q_head_stride);
+  d.page = units(a->page_stride); d.head = units(a->head_stride); d.row = units(a->row_stride);
+  d.new_batch = units(a->new_batch_stride); d.new_head = units(a->new_head_stride);
+  d.out_batch = units(a->out_batch_stride); d.out_head = units(a->out_head_stride);
   d.lse_batch = a->lse_batch_stride; d.lse_head = a->lse_head_stride;
   d.n_kv_heads = a->n_kv_heads; d.group = a->n_q_heads / a->n_kv_heads; d.dh = a->head_dim;
+  // key / page_size by one multiplication: m = ceil(2^(32 + s) / page_size) - 2^32 with s = ceil(log2 page_size)
+  const unsigned ps = a->page_size > 0 ? (unsigned)a->page_size : 1u;
+  while ((1ull << d.page_shift) < ps) ++d.page_shift;
+  d.page_mul = (unsigned)((((1ull << d.page_shift) - ps) << 32) / ps + (ps == (1ull << d.page_shift) ? 0 : 1));
+  d.aligned = a->page_size % kPiece == 0;
   d.page_size = a->page_size; d.max_blocks = a->max_blocks; d.n_pages = a->n_pages;
-  d.cap = a->page_size > 0 ? (long long)a->max_blocks * a->page_size : a->max_keys;
-  if (d.cap > 0x7fffff00ll) d.cap = 0x7fffff00ll;                                            // keys are counted in 32 bits
+  long long bound = a->page_size > 0 ? (long long)a->max_blocks * a->page_size : a->max_keys;
+  if (bound > 0x7fffff00ll) bound = 0x7fffff00ll;                                            // keys are counted in 32 bits
+  // and so are the blocks of 32 keys of a batch, and of a request over all heads
+  if ((bound / 32 + 1) * std::max(a->batch, a->n_q_heads) > 0x7fffffffll) return LIGHTKV_ERR_UNSUPPORTED;
+  d.cap = (int)bound;
   const double scale = a->scale != 0.f ? a->scale : 1.0 / sqrt((double)a->head_dim);
   d.scale_log2 = (float)(scale * 1.4426950408889634);
-  long long bound = d.cap;
   if (a->max_keys > 0 && a->max_keys < bound) bound = a->max_keys;
-  if (launch_decode(d, a->dtype, a->batch, (int)bound, static_cast<cudaStream_t>(a->stream)) != cudaSuccess) return LIGHTKV_ERR_CUDA;
-  return LIGHTKV_OK;
+  const cudaError_t e = with_variant(a->dtype, d.group, d.dh, [&](auto v) {
+    return launch_form<decltype(v)>(d, a->batch, (int)bound, a->workspace, static_cast<cudaStream_t>(a->stream));
+  });
+  return e == cudaSuccess ? LIGHTKV_OK : LIGHTKV_ERR_CUDA;
 }
 
 }  // extern "C"
