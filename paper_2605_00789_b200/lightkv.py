@@ -2,7 +2,8 @@
 
 PyTorch is used for device memory and streams: tensors are handed over as data pointers plus element
 strides, the current CUDA stream as a raw handle.  No arithmetic of the method happens here.  Plans go
-through ctypes; the calls of every layer are marshalled natively (csrc/binding.c, module _binding).
+through ctypes; the calls of every layer are marshalled natively (csrc/binding.c, module _binding), and so are the calls that
+serve a compacted cache (csrc/serving_binding.cpp, module _serving).
 """
 from __future__ import annotations
 
@@ -285,11 +286,9 @@ def _binding():
         except ImportError as exc:
             raise LightKVError(f"_binding.so is missing: build it first (python -c 'import __graft_entry__ as g; g.build()'): {exc}")
         address = lambda f: C.cast(f, C.c_void_p).value
-        native.bind(tuple(address(f) for f in (lib.lightkv_compress_layer, lib.lightkv_compress_layer_builtin_ws,
-                                               lib.lightkv_compact_kv, lib.lightkv_decode_attention, lib.lightkv_append_kv,
-                                               lib.lightkv_assign_pages)),
-                    _fail, _fork_join, torch._C._cuda_getCurrentRawStream, torch.cuda.current_device,
-                    (torch.bfloat16, torch.float32, torch.int32, torch.int64))
+        native.bind(address(lib.lightkv_compress_layer), address(lib.lightkv_compress_layer_builtin_ws),
+                    address(lib.lightkv_compact_kv), _fail, _fork_join, torch._C._cuda_getCurrentRawStream,
+                    torch.cuda.current_device)
         _BINDING = native
     return _BINDING
 
@@ -338,24 +337,25 @@ def pages_workspace_bytes(batch: int) -> int:
     return n + 256
 
 
-def decode_attention(q, k_cache, v_cache, n_keys, out, **kw) -> None:
-    """lightkv_decode_attention.  q, out [B,H,dh]; n_keys [B] int32.  With block_table [B,max_blocks] int32 the caches are
-    page pools [n_pages,H_kv,page_size,dh], else [B,H_kv,N,dh] (any strides with a contiguous last dimension, the same for K
-    and V).  Keywords: workspace (required: a tensor of decode_workspace_bytes bytes), lse [B,H] fp32, k_new / v_new
-    [B,H_kv,dh] (rows that stand for key n_keys - 1 and are written to the cache), scale (default 1 / sqrt(dh)), max_keys (an
-    upper bound of n_keys, paged), status [1] int32, stream.  All tensors are on the current device."""
-    (_BINDING or _binding()).decode_attention(q, k_cache, v_cache, n_keys, out, **kw)
+_SERVING = ("decode_attention", "append_kv", "assign_pages")
 
 
-def append_kv(k_new, v_new, k_cache, v_cache, slot_map, **kw) -> None:
-    """lightkv_append_kv.  k_new, v_new [T,H_kv,dh]; caches [n_pages,H_kv,page_size,dh]; slot_map [T] int64, negative: skipped.
-    Keywords: status [1] int32, stream."""
-    (_BINDING or _binding()).append_kv(k_new, v_new, k_cache, v_cache, slot_map, **kw)
+def __getattr__(name):
+    """The serving calls are functions of the native module _serving (csrc/serving_binding.cpp), imported when one is first
+    asked for: it is linked to torch, which this module does not import."""
+    if name not in _SERVING:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    import torch  # noqa: F401  (its libraries)
+    try:
+        from . import _serving as native
+    except ImportError as exc:
+        raise LightKVError(f"_serving.so is missing: build it first (python -c 'import __graft_entry__ as g; g.build()'): {exc}")
 
+    def load():
+        lib = library()
+        native.bind(*(C.cast(getattr(lib, "lightkv_" + f), C.c_void_p).value for f in _SERVING))
 
-def assign_pages(seq_len, block_table, free_pages, n_free, **kw) -> None:
-    """lightkv_assign_pages.  seq_len [B] int32, block_table [B,max_blocks] int32, free_pages [n_pages] int32, n_free [1] int32.
-    Keywords: page_size and workspace (required; a tensor of pages_workspace_bytes bytes), add, held [B] int32, seq_len_out [B]
-    (default: in place of held, or of seq_len where none is given), n_free_out [1] (default: in place of n_free), slot_map
-    [n_slots] int64, slot_start [B+1] int32, slot_stride, status [1] int32, stream."""
-    (_BINDING or _binding()).assign_pages(seq_len, block_table, free_pages, n_free, **kw)
+    native.setup(load, _fail)
+    for f in _SERVING:
+        globals()[f] = getattr(native, f)
+    return globals()[name]
