@@ -117,6 +117,14 @@ __host__ __device__ inline int div_magic(int n, unsigned int m) {
 #endif
 }
 
+// floor(n / d) = (umulhi(n, m) + n) >> s for n < 2^31 and any d >= 1: s = ceil(log2 d), m = ceil(2^(32 + s) / d) - 2^32 (the method of
+// Granlund and Montgomery; umulhi(n, m) < n, so that the sum fits 32 bits)
+inline void page_divider(unsigned int d, unsigned int* m, int* s) {
+  *s = 0;
+  while ((1ull << *s) < d) ++*s;
+  *m = (unsigned int)((((1ull << *s) - d) << 32) / d + ((1ull << *s) != d));
+}
+
 // ---- 16-byte vector access and element conversion -----------------------------------------------
 template <typename T> struct Vec;                      // elements per 16 bytes
 template <> struct Vec<__nv_bfloat16> { static constexpr int n = 8; };

@@ -1087,10 +1087,7 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   d.out_batch = units(a->out_batch_stride); d.out_head = units(a->out_head_stride);
   d.lse_batch = a->lse_batch_stride; d.lse_head = a->lse_head_stride;
   d.n_kv_heads = a->n_kv_heads; d.group = a->n_q_heads / a->n_kv_heads; d.dh = a->head_dim;
-  // key / page_size by one multiplication: m = ceil(2^(32 + s) / page_size) - 2^32 with s = ceil(log2 page_size)
-  const unsigned ps = a->page_size > 0 ? (unsigned)a->page_size : 1u;
-  while ((1ull << d.page_shift) < ps) ++d.page_shift;
-  d.page_mul = (unsigned)((((1ull << d.page_shift) - ps) << 32) / ps + (ps == (1ull << d.page_shift) ? 0 : 1));
+  page_divider(a->page_size > 0 ? (unsigned)a->page_size : 1u, &d.page_mul, &d.page_shift);
   d.aligned = a->page_size % kPiece == 0;
   d.page_size = a->page_size; d.max_blocks = a->max_blocks; d.n_pages = a->n_pages;
   long long bound = a->page_size > 0 ? (long long)a->max_blocks * a->page_size : a->max_keys;

@@ -7,30 +7,30 @@
 // its place alone: a moved page is read once where it stands now (a free entry, or the table row of a request that shrinks) and
 // written once where it belongs (the stack above n_free, or the row of a request that grows).  Neither side touches what the
 // other reads: entries above n_free are written only if no free page is taken.
-// One CTA finds the sums (a few microseconds of latency); with few slots it also moves the pages and writes the slots, else a
-// second kernel over the whole GPU does.
+// What is left is latency.  Few slots and up to kPageRows requests: a cluster whose CTAs all find the sums, so that none waits for
+// another's, and share the moves; the first one writes the lengths, once all have read theirs (they may be the same array).
+// Else one CTA finds the sums and a second kernel over the whole GPU moves pages and writes slots.
+//   us a call: 256 requests that grow by a token 4.5 -> XX, 64 that give back half of 65 pages on average 6.5 -> XX (one CTA -> a
+//   cluster of eight), 128 that are admitted with 438 000 slots 12.4 -> XX (rows searched in L2 -> in shared memory)
 #include <limits.h>
 
 #include "launch.h"
+#include "tc_common.cuh"
 
 namespace lkv {
 
 namespace {
 
-struct PageRow {                       // one request
-  int held, have, need;                // tokens; pages held, pages afterwards (have where it was not served)
-  int served;
-  long long gone_at, grow_at, fresh_at;          // exclusive prefix sums over the requests in front
-  long long fresh;                     // new tokens asked for
-};
-struct PageTotals { long long n_free, stacked, left, taken, fresh; };
-
-constexpr int kPageThreads = 1024;
-constexpr int kPageRowsOnChip = 768;   // requests whose rows fit the shared memory a CTA has without asking
-constexpr size_t kTotalsBytes = 256;
+// Threads of a CTA; each looks at up to kPerThread requests (with a request a thread, 1024 threads, the shuffles of the sums alone
+// took a microsecond of the SM).
+constexpr int kPageThreads = 256, kPerThread = 4;
+constexpr int kPageRows = kPageThreads * kPerThread;         // requests that are summed at once, and whose rows are kept on chip
+constexpr int kPageCluster = 8;
+constexpr int kPageSlots = 65536;      // most slots a cluster writes
 
 struct PageArgs {
   int batch, page_size, max_blocks, n_pages, add;
+  unsigned page_mul; int page_shift;   // n / page_size = (umulhi(n, page_mul) + n) >> page_shift for n < 2^31
   const int* held; const int* seq_len;
   int* seq_len_out; int* block_table; int* free_pages;
   const int* n_free; int* n_free_out;
@@ -38,196 +38,263 @@ struct PageArgs {
   int n_slots, slot_stride;
   int* slot_start;
   uint32_t* status;
-  PageRow* rows;                       // workspace
-  PageTotals* totals;
+  unsigned char* workspace;
 };
 
-struct Sums { long long gone, grow, fresh; };
-__device__ __forceinline__ Sums add(const Sums& a, const Sums& b) { return {a.gone + b.gone, a.grow + b.grow, a.fresh + b.fresh}; }
-__device__ __forceinline__ Sums shfl_up(const Sums& a, int d) {
-  return {__shfl_up_sync(0xffffffffu, a.gone, d), __shfl_up_sync(0xffffffffu, a.grow, d), __shfl_up_sync(0xffffffffu, a.fresh, d)};
-}
+__device__ __forceinline__ unsigned pages_of(const PageArgs& a, unsigned n) { return (__umulhi(n, a.page_mul) + n) >> a.page_shift; }   // whole ones
 
-// What request b asks for; `status` collects its complaints.
-__device__ __forceinline__ Sums page_request(const PageArgs& a, int b, PageRow& r, long long& want, int& base, unsigned& status) {
-  const long long room = (long long)a.max_blocks * a.page_size;
-  long long held = a.held ? max(a.held[b], 0) : 0;
-  base = a.seq_len[b];
-  want = base < 0 ? 0 : (long long)base + a.add;
-  if (held > room) { held = room; status |= LIGHTKV_STATUS_COUNT; }
-  r.held = (int)held;
-  r.have = (int)((held + a.page_size - 1) / a.page_size);
-  r.fresh = max(want - held, 0ll);
-  r.served = want <= room;
-  if (!r.served) status |= LIGHTKV_STATUS_COUNT;
-  r.need = r.served ? (int)((want + a.page_size - 1) / a.page_size) : r.have;
-  return {max(r.have - r.need, 0), max(r.need - r.have, 0), r.fresh};
-}
-
-// The sums over all requests, their rows, lengths and offsets, and the new height of the stack.  All threads of one CTA.
-__device__ void plan_pages(const PageArgs& a, PageRow* rows, PageTotals* totals) {
-  __shared__ Sums warp_sum[32];
-  __shared__ long long all_gone;
-  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  unsigned status = 0;
-  long long n_free = *a.n_free;
-  if (n_free < 0 || n_free > a.n_pages) { n_free = n_free < 0 ? 0 : a.n_pages; status |= LIGHTKV_STATUS_COUNT; }
-  Sums carry = {0, 0, 0};
-  long long stacked = 0, taken = 0;
-  if (a.batch > kPageThreads) {        // the height of the stack is needed before the first chunk
-    long long gone = 0;
-    for (int b = t; b < a.batch; b += kPageThreads) {
-      PageRow r; long long want; int base; unsigned ignore = 0;
-      gone += page_request(a, b, r, want, base, ignore).gone;
-    }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) gone += __shfl_xor_sync(0xffffffffu, gone, d);
-    if (t == 0) all_gone = 0;
-    __syncthreads();
-    if (lane == 0) atomicAdd(reinterpret_cast<unsigned long long*>(&all_gone), (unsigned long long)gone);
-    __syncthreads();
-    stacked = n_free + all_gone;
+struct PageTotals { long long fresh; unsigned n_free, stacked, left, taken; };
+// What is kept of the requests, in shared memory or in the workspace.  (The host has seen to it that all blocks of the table are
+// counted in 32 bits.)
+struct PageRows {
+  long long* fresh_at;                 // exclusive sums of the new tokens asked for, and behind the last the whole
+  unsigned *gone_at, *grow_at;         // exclusive sums of the pages given back and asked for
+  int *held, *have, *need;             // tokens; pages held; pages afterwards (have and ~have where it was not served)
+  __host__ __device__ static constexpr size_t bytes(int batch) { return size_t(batch + 1) * 8 + size_t(batch) * 20; }
+  __device__ __forceinline__ PageRows(unsigned char* p, int batch) {
+    fresh_at = reinterpret_cast<long long*>(p);
+    gone_at = reinterpret_cast<unsigned*>(fresh_at + batch + 1);
+    grow_at = gone_at + batch;
+    held = reinterpret_cast<int*>(grow_at + batch);
+    have = held + batch;
+    need = have + batch;
   }
-  for (int b0 = 0; b0 < a.batch; b0 += kPageThreads) {
-    const int b = b0 + t;
-    PageRow r = {};
-    long long want = 0;
-    int base = 0;
-    Sums own = {0, 0, 0};
-    if (b < a.batch) own = page_request(a, b, r, want, base, status);
-    Sums sum = own;
+};
+
+struct Sums { long long fresh; unsigned gone, grow; };
+__device__ __forceinline__ Sums add(const Sums& a, const Sums& b) { return {a.fresh + b.fresh, a.gone + b.gone, a.grow + b.grow}; }
+__device__ __forceinline__ Sums scan(Sums a) {               // inclusive, over a warp
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const Sums o = shfl_up(sum, d);
-      if (lane >= d) sum = add(sum, o);
-    }
-    if (lane == 31) warp_sum[warp] = sum;
-    __syncthreads();
-    if (warp == 0) {
-      Sums v = warp_sum[lane];
+  for (int d = 1; d < 32; d <<= 1) {
+    const Sums o = {__shfl_up_sync(0xffffffffu, a.fresh, d), __shfl_up_sync(0xffffffffu, a.gone, d), __shfl_up_sync(0xffffffffu, a.grow, d)};
+    if (int(threadIdx.x & 31) >= d) a = add(a, o);
+  }
+  return a;
+}
+
+struct Request { int held, have, need, base; long long want; bool fits; };
+__device__ __forceinline__ Sums page_request(const PageArgs& a, int b, Request& r, unsigned& status) {
+  const int room = a.max_blocks * a.page_size;
+  r.held = a.held ? max(a.held[b], 0) : 0;
+  r.base = a.seq_len[b];
+  r.want = r.base < 0 ? 0 : (long long)r.base + a.add;
+  if (r.held > room) { r.held = room; status |= LIGHTKV_STATUS_COUNT; }
+  r.have = r.held ? pages_of(a, r.held - 1) + 1 : 0;
+  r.fits = r.want <= room;
+  if (!r.fits) status |= LIGHTKV_STATUS_COUNT;
+  r.need = r.fits ? (r.want ? pages_of(a, unsigned(r.want) - 1u) + 1 : 0) : r.have;
+  return {max(r.want - r.held, 0ll), unsigned(max(r.have - r.need, 0)), unsigned(max(r.need - r.have, 0))};
+}
+
+// The sums over all requests, their rows, lengths and offsets, and the new height of the stack.  All threads of one CTA; `before`
+// is called when everything has been read and before anything that a caller may have given as input is written, which
+// `writes` CTAs do.
+template <typename F>
+__device__ void plan_pages(const PageArgs& a, const PageRows& rows, PageTotals& totals, bool writes, F before) {
+  constexpr int WARPS = kPageThreads / 32;
+  __shared__ Sums warp_sum[2][WARPS];
+  __shared__ unsigned long long shared_max;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const bool chunks = a.batch > kPageRows;
+  const int per = chunks ? kPerThread : (a.batch + kPageThreads - 1) / kPageThreads;         // consecutive requests of a thread
+  unsigned status = 0;
+  int n = *a.n_free;
+  Request r[kPerThread];
+  Sums own[kPerThread];
+  auto read = [&](int b0) {
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const Sums o = shfl_up(v, d);
-        if (lane >= d) v = add(v, o);
-      }
-      warp_sum[lane] = v;
+    for (int j = 0; j < kPerThread; ++j) {
+      const int b = b0 + t * per + j;
+      own[j] = {0, 0, 0};
+      if (j < per && b < a.batch) own[j] = page_request(a, b, r[j], status);
     }
+  };
+  if (!chunks) {
+    read(0);
+    if (a.slot_map)                    // the pages of the next tokens, which slots may want
+#pragma unroll
+      for (int j = 0; j < kPerThread; ++j)
+        if (j < per && t * per + j < a.batch && own[j].fresh > 0 && r[j].held < a.max_blocks * a.page_size)
+          prefetch_l2(a.block_table + (size_t)(t * per + j) * a.max_blocks + pages_of(a, r[j].held));
+  }
+  if (n < 0 || n > a.n_pages) { n = n < 0 ? 0 : a.n_pages; status |= LIGHTKV_STATUS_COUNT; }
+  const unsigned n_free = n;
+  if (t < 32 && 32 * t < int(n_free)) prefetch_l2(a.free_pages + n_free - 1 - 32 * t);       // what is popped first
+  unsigned stacked = 0;
+  if (chunks) {                        // the height of the stack is needed before the first chunk
+    unsigned gone = 0;
+    for (int b = t; b < a.batch; b += kPageThreads) {
+      unsigned ignore = 0;
+      Request q;
+      gone += page_request(a, b, q, ignore).gone;
+    }
+    gone = __reduce_add_sync(0xffffffffu, gone);
+    if (t == 0) shared_max = 0;
     __syncthreads();
-    const Sums chunk = warp_sum[31];
-    sum = add(sum, carry);
-    if (warp > 0) sum = add(sum, warp_sum[warp - 1]);        // inclusive, over all requests
-    if (a.batch <= kPageThreads) stacked = n_free + chunk.gone;
-    if (b < a.batch) {
-      const bool short_of = own.grow > 0 && sum.grow > stacked;
-      if (short_of) { status |= LIGHTKV_STATUS_NO_PAGES; r.served = 0; r.need = r.have; }
-      r.gone_at = sum.gone - own.gone;
-      r.grow_at = sum.grow - own.grow;
-      r.fresh_at = sum.fresh - own.fresh;
-      if (own.grow > 0 && !short_of) taken = sum.grow;       // the last one served has the largest
-      rows[b] = r;
-      a.seq_len_out[b] = base < 0 ? base : r.served ? (int)want : r.held;
-      if (a.slot_start) {
-        a.slot_start[b] = (int)min(r.fresh_at, (long long)INT_MAX);
-        if (b == a.batch - 1) a.slot_start[a.batch] = (int)min(sum.fresh, (long long)INT_MAX);
+    if (lane == 0) atomicAdd(&shared_max, (unsigned long long)gone);
+    __syncthreads();
+    stacked = n_free + unsigned(shared_max);
+    __syncthreads();
+  }
+  Sums carry = {0, 0, 0};
+  unsigned taken = 0;
+  int flip = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kPageRows, flip ^= 1) {
+    if (chunks) read(b0);
+    Sums mine = own[0];
+#pragma unroll
+    for (int j = 1; j < kPerThread; ++j) mine = add(mine, own[j]);
+    const Sums sum = scan(mine);
+    if (lane == 31) warp_sum[flip][warp] = sum;
+    __syncthreads();
+    Sums at = {carry.fresh + sum.fresh - mine.fresh, carry.gone + sum.gone - mine.gone, carry.grow + sum.grow - mine.grow}, chunk = {0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+      const Sums w = warp_sum[flip][i];
+      if (i < warp) at = add(at, w);
+      chunk = add(chunk, w);
+    }
+    if (!chunks) {
+      stacked = n_free + chunk.gone;
+      before();
+    }
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) {
+      const int b = b0 + t * per + j;
+      if (j >= per || b >= a.batch) break;
+      const Sums next = add(at, own[j]);
+      const bool served = r[j].fits && (own[j].grow == 0 || next.grow <= stacked);
+      if (r[j].fits && !served) status |= LIGHTKV_STATUS_NO_PAGES;
+      if (own[j].grow > 0 && served) taken = next.grow;      // the last one served has the largest
+      rows.fresh_at[b] = at.fresh;
+      rows.gone_at[b] = at.gone;
+      rows.grow_at[b] = at.grow;
+      rows.held[b] = r[j].held;
+      rows.have[b] = r[j].have;
+      rows.need[b] = served ? r[j].need : ~r[j].have;
+      if (b == a.batch - 1) rows.fresh_at[a.batch] = next.fresh;
+      if (writes) {
+        a.seq_len_out[b] = r[j].base < 0 ? r[j].base : served ? (int)r[j].want : r[j].held;
+        if (a.slot_start) {
+          a.slot_start[b] = (int)min(at.fresh, (long long)INT_MAX);
+          if (b == a.batch - 1) a.slot_start[a.batch] = (int)min(next.fresh, (long long)INT_MAX);
+        }
+        if (a.slot_map && own[j].fresh > 0) {
+          const long long end = a.slot_stride ? (long long)b * a.slot_stride + min(own[j].fresh, (long long)a.slot_stride) : next.fresh;
+          if (end > a.n_slots || (a.slot_stride && own[j].fresh > a.slot_stride)) status |= LIGHTKV_STATUS_COUNT;
+        }
       }
-      if (a.slot_map) {
-        const long long end = a.slot_stride ? (long long)b * a.slot_stride + min(r.fresh, (long long)a.slot_stride) : sum.fresh;
-        if (r.fresh > 0 && (end > a.n_slots || (a.slot_stride && r.fresh > a.slot_stride))) status |= LIGHTKV_STATUS_COUNT;
-      }
+      at = next;
     }
     carry = add(carry, chunk);
+  }
+  if (carry.grow <= stacked && !chunks) {
+    taken = carry.grow;                // all were served (the others ask for nothing)
     __syncthreads();
+  } else {
+    taken = __reduce_max_sync(0xffffffffu, taken);
+    if (t == 0) shared_max = 0;
+    __syncthreads();
+    if (lane == 0) atomicMax(&shared_max, (unsigned long long)taken);
+    __syncthreads();
+    taken = unsigned(shared_max);
   }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) taken = max(taken, __shfl_xor_sync(0xffffffffu, taken, d));
-  if (t == 0) all_gone = 0;
-  __syncthreads();
-  if (lane == 0) atomicMax(reinterpret_cast<unsigned long long*>(&all_gone), (unsigned long long)taken);
-  __syncthreads();
-  taken = all_gone;
-  if (t == 0) {
-    long long left = stacked - taken;
-    if (left > a.n_pages) { left = a.n_pages; status |= LIGHTKV_STATUS_COUNT; }      // page numbers held twice
-    *totals = {n_free, stacked, left, taken, carry.fresh};
-    *a.n_free_out = (int)left;
+  unsigned left = stacked - taken;
+  if (left > unsigned(a.n_pages)) { left = a.n_pages; status |= LIGHTKV_STATUS_COUNT; }      // page numbers held twice
+  totals = {carry.fresh, n_free, stacked, left, taken};      // (in every thread)
+  if (writes) {
+    if (t == 0) *a.n_free_out = (int)left;
+    if (a.status && status) atomicOr(a.status, status);
   }
-  if (a.status && status) atomicOr(a.status, status);
-  __syncthreads();
 }
 
-// last request whose prefix sum is at most `at` among those with the sum non-decreasing: the one that entry `at` belongs to
-template <typename Get>
-__device__ __forceinline__ int find_row(int batch, long long at, Get get) {
-  int lo = 0, hi = batch;              // get(lo) <= at < get(hi)
+// last row whose sum is at most `at`: the one that entry `at` belongs to
+template <typename T>
+__device__ __forceinline__ int find_row(const T* sums, int batch, T at) {
+  int lo = 0, hi = batch;              // sums[lo] <= at < sums[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (get(mid) <= at) lo = mid; else hi = mid;
+    if (sums[mid] <= at) lo = mid; else hi = mid;
   }
   return lo;
 }
 
-__device__ __forceinline__ int released_page(const PageArgs& a, const PageRow* rows, long long i) {
-  const int b = find_row(a.batch, i, [&](int m) { return rows[m].gone_at; });
-  const long long at = rows[b].need + (i - rows[b].gone_at);
-  return at < a.max_blocks ? a.block_table[(size_t)b * a.max_blocks + at] : -1;
+__device__ __forceinline__ int released_page(const PageArgs& a, const PageRows& rows, unsigned i) {
+  const int b = find_row(rows.gone_at, a.batch, i);
+  const unsigned need = rows.need[b] < 0 ? ~rows.need[b] : rows.need[b], at = need + (i - rows.gone_at[b]);
+  return at < unsigned(a.max_blocks) ? a.block_table[(size_t)b * a.max_blocks + at] : -1;
 }
 // the k-th page that is taken
-__device__ __forceinline__ int taken_page(const PageArgs& a, const PageRow* rows, const PageTotals& s, long long k) {
-  const long long i = s.stacked - 1 - k;
+__device__ __forceinline__ int taken_page(const PageArgs& a, const PageRows& rows, const PageTotals& s, unsigned k) {
+  const unsigned i = s.stacked - 1 - k;
   return i < s.n_free ? a.free_pages[i] : released_page(a, rows, i - s.n_free);
 }
 
 // The moves and the slots, shared by `threads` threads of which this is number `id`.
-__device__ void move_pages(const PageArgs& a, const PageRow* rows, const PageTotals& s, long long id, long long threads) {
-  for (long long i = s.n_free + id; i < s.left; i += threads) a.free_pages[i] = released_page(a, rows, i - s.n_free);
-  for (long long k = id; k < s.taken; k += threads) {
-    const int b = find_row(a.batch, k, [&](int m) { return rows[m].grow_at; });
-    a.block_table[(size_t)b * a.max_blocks + rows[b].have + (k - rows[b].grow_at)] = taken_page(a, rows, s, k);
-  }
-  if (!a.slot_map) return;
+__device__ void move_pages(const PageArgs& a, const PageRows& rows, const PageTotals& s, unsigned id, unsigned threads) {
   unsigned status = 0;
-  for (long long t = id; t < a.n_slots; t += threads) {
-    long long slot = -1, i = 0;
-    int b = a.batch;
-    if (a.slot_stride) {
-      b = (int)(t / a.slot_stride);
-      i = t - (long long)b * a.slot_stride;
-    } else if (t < s.fresh) {
-      b = find_row(a.batch, t, [&](int m) { return rows[m].fresh_at; });
-      i = t - rows[b].fresh_at;
-    }
-    if (b < a.batch) {
-      const PageRow& r = rows[b];
-      if (r.served && i < r.fresh) {
-        const unsigned p = unsigned(r.held) + unsigned(i), block = p / unsigned(a.page_size);
-        const int page = (int)block < r.have ? a.block_table[(size_t)b * a.max_blocks + block]
-                                             : taken_page(a, rows, s, r.grow_at + ((int)block - r.have));
+  if (a.slot_map)
+    for (long long t = id; t < a.n_slots; t += threads) {
+      long long slot = -1, i = 0;
+      int b = a.batch;
+      if (a.slot_stride) {
+        b = int(unsigned(t) / unsigned(a.slot_stride));
+        i = t - (long long)b * a.slot_stride;
+      } else if (t < s.fresh) {
+        b = find_row(rows.fresh_at, a.batch, t);
+        i = t - rows.fresh_at[b];
+      }
+      if (b < a.batch && rows.need[b] >= 0 && i < rows.fresh_at[b + 1] - rows.fresh_at[b]) {
+        const unsigned p = unsigned(rows.held[b]) + unsigned(i), block = pages_of(a, p);
+        const int page = (int)block < rows.have[b] ? a.block_table[(size_t)b * a.max_blocks + block]
+                                                   : taken_page(a, rows, s, rows.grow_at[b] + (block - rows.have[b]));
         if (unsigned(page) < unsigned(a.n_pages)) slot = (long long)page * a.page_size + (p - block * a.page_size);
         else status |= LIGHTKV_STATUS_PAGE;
       }
+      a.slot_map[t] = slot;
     }
-    a.slot_map[t] = slot;
+  id = threads - 1 - id;               // (pages move while others write slots)
+  for (unsigned i = s.n_free + id; i < s.left; i += threads) a.free_pages[i] = released_page(a, rows, i - s.n_free);
+  for (unsigned k = id; k < s.taken; k += threads) {
+    const int b = find_row(rows.grow_at, a.batch, k);
+    a.block_table[(size_t)b * a.max_blocks + rows.have[b] + (k - rows.grow_at[b])] = taken_page(a, rows, s, k);
   }
   if (status && a.status) atomicOr(a.status, status);
 }
 
 __global__ void __launch_bounds__(kPageThreads) pages_kernel(const __grid_constant__ PageArgs a) {
-  __shared__ PageRow on_chip[kPageRowsOnChip];
-  __shared__ PageTotals totals;
+  __shared__ __align__(8) unsigned char on_chip[PageRows::bytes(kPageRows)];
   grid_dependency_sync();
-  PageRow* rows = a.batch <= kPageRowsOnChip ? on_chip : a.rows;
-  plan_pages(a, rows, &totals);
-  move_pages(a, rows, totals, threadIdx.x, kPageThreads);
+  const PageRows rows(on_chip, a.batch);
+  const unsigned rank = tc::cluster_ctarank();
+  PageTotals totals;
+  plan_pages(a, rows, totals, rank == 0, [&] {               // (what was read has arrived: nothing to release)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    if (rank == 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  });
+  move_pages(a, rows, totals, rank * kPageThreads + threadIdx.x, kPageCluster * kPageThreads);
+  if (rank != 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 __global__ void __launch_bounds__(kPageThreads) pages_plan_kernel(const __grid_constant__ PageArgs a) {
   grid_dependency_sync();
-  plan_pages(a, a.rows, a.totals);
+  PageTotals totals;
+  plan_pages(a, PageRows(a.workspace + 256, a.batch), totals, true, [] {});
+  if (threadIdx.x == 0) *reinterpret_cast<PageTotals*>(a.workspace) = totals;
 }
 
 __global__ void __launch_bounds__(256) pages_move_kernel(const __grid_constant__ PageArgs a) {
+  __shared__ __align__(8) unsigned char on_chip[PageRows::bytes(kPageRows)];
   grid_dependency_sync();
-  move_pages(a, a.rows, *a.totals, blockIdx.x * 256ll + threadIdx.x, gridDim.x * 256ll);
+  unsigned char* from = a.workspace + 256;
+  const PageTotals totals = *reinterpret_cast<const PageTotals*>(a.workspace);
+  if (a.batch <= kPageRows) {
+    const int words = int(PageRows::bytes(a.batch) / 4);
+    for (int i = threadIdx.x; i < words; i += 256) reinterpret_cast<int*>(on_chip)[i] = reinterpret_cast<const int*>(from)[i];
+    __syncthreads();
+    from = on_chip;
+  }
+  move_pages(a, PageRows(from, a.batch), totals, blockIdx.x * 256u + threadIdx.x, gridDim.x * 256u);
 }
 
 // ---- rows of new tokens ---------------------------------------------------------------------------------------------------
@@ -285,7 +352,7 @@ using namespace lkv;
 
 extern "C" {
 
-size_t lightkv_pages_workspace(int32_t batch) { return batch < 0 ? 0 : kTotalsBytes + size_t(batch) * sizeof(PageRow); }
+size_t lightkv_pages_workspace(int32_t batch) { return batch < 0 ? 0 : 256 + PageRows::bytes(batch); }
 
 int lightkv_assign_pages(const lightkv_pages_args_t* a) {
   if (!a || a->struct_size != sizeof(lightkv_pages_args_t)) return LIGHTKV_ERR_INVALID_ARG;
@@ -294,6 +361,7 @@ int lightkv_assign_pages(const lightkv_pages_args_t* a) {
   if (!a->seq_len || !a->seq_len_out || !a->block_table || !a->free_pages || !a->n_free || !a->n_free_out || !a->workspace)
     return LIGHTKV_ERR_INVALID_ARG;
   if ((long long)a->max_blocks * a->page_size > INT_MAX) return LIGHTKV_ERR_INVALID_ARG;     // lengths are 32-bit
+  if ((long long)a->max_blocks * a->batch + a->n_pages > INT_MAX) return LIGHTKV_ERR_UNSUPPORTED;            // pages are counted in 32 bits
   if (!a->slot_map != !a->n_slots || (a->slot_stride && !a->slot_map)) return LIGHTKV_ERR_INVALID_ARG;
   if (a->slot_map && !aligned(a->slot_map, 8)) return LIGHTKV_ERR_INVALID_ARG;
   if (a->block_table == a->free_pages || a->seq_len_out == a->n_free_out || a->seq_len_out == a->slot_start) return LIGHTKV_ERR_INVALID_ARG;
@@ -304,14 +372,13 @@ int lightkv_assign_pages(const lightkv_pages_args_t* a) {
   p.free_pages = a->free_pages; p.n_free = a->n_free; p.n_free_out = a->n_free_out;
   p.slot_map = reinterpret_cast<long long*>(a->slot_map); p.n_slots = a->n_slots; p.slot_stride = a->slot_stride;
   p.slot_start = a->slot_start; p.status = a->status;
-  p.totals = static_cast<PageTotals*>(a->workspace);
-  p.rows = reinterpret_cast<PageRow*>(static_cast<char*>(a->workspace) + kTotalsBytes);
+  p.workspace = static_cast<unsigned char*>(a->workspace);
+  page_divider((unsigned)a->page_size, &p.page_mul, &p.page_shift);
   cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
-  if (a->n_slots <= 4 * kPageThreads && a->batch <= kPageRowsOnChip)
-    return launch_kernel(pages_kernel, dim3(1), dim3(kPageThreads), 0, stream, 1, p) == cudaSuccess ? LIGHTKV_OK : LIGHTKV_ERR_CUDA;
-  const unsigned grid = 4u * sm_count();
+  if (a->n_slots <= kPageSlots && a->batch <= kPageRows)
+    return launch_kernel(pages_kernel, dim3(kPageCluster), dim3(kPageThreads), 0, stream, kPageCluster, p) == cudaSuccess ? LIGHTKV_OK : LIGHTKV_ERR_CUDA;
   if (launch_kernel(pages_plan_kernel, dim3(1), dim3(kPageThreads), 0, stream, 1, p) != cudaSuccess ||
-      launch_kernel(pages_move_kernel, dim3(grid), dim3(256), 0, stream, 1, p) != cudaSuccess)
+      launch_kernel(pages_move_kernel, dim3(4u * sm_count()), dim3(256), 0, stream, 1, p) != cudaSuccess)
     return LIGHTKV_ERR_CUDA;
   return LIGHTKV_OK;
 }
