@@ -158,15 +158,11 @@ struct Walk {
 
 // fp32, K: rows are copied in whole lines, 32 consecutive 16-byte units per instruction, and land where the lane that needs them
 // reads them: unit x of row r belongs to lane 4 (r % 8) + x % 4 as its unit (r / 8) U / 4 + x / 4 of U.
-template <int CH>
-struct CopyMap {
-  static constexpr int R = 32 / CH, N = kPiece / R;          // rows per instruction, instructions
-  // K: where this lane's unit of instruction n lands, less 512 (n R / 8) CH / 4 + 64 (n R % 8 rounded down to even)
-  static __device__ __forceinline__ uint32_t k_lane(int odd) {
-    const int lane = threadIdx.x & 31, x = lane % CH, lr = lane / CH + odd;
-    return (x / 4) * 512 + (((lr * 4 + x % 4) ^ ((x / 4 & 1) << 2)) * 16);
-  }
-};
+// This lane's unit of row `odd` (0 or 1) of K lands there; 64 bytes further for every row further, 512 U / 4 behind eight.
+__device__ __forceinline__ uint32_t k_lane(int odd) {
+  const int lane = threadIdx.x & 31;
+  return (lane / 4) * 512 + (((odd * 4 + lane % 4) ^ ((lane / 4 & 1) << 2)) * 16);
+}
 // the slot that a lane reads its K piece kc from
 __device__ __forceinline__ int k_slot(int kc) { return (threadIdx.x & 31) ^ ((kc & 1) << 2); }
 
@@ -381,29 +377,30 @@ struct WarpFp32 {
     for (int i = 0; i < RL; ++i) l[i] = 0.f;
   }
   __device__ __forceinline__ void fetch(const DecodeArgs& a, const Walk& w, uint32_t stage) {
-    constexpr int CH = 32;                                   // units of 128 channels; wider rows: one half after the other
-    using M = CopyMap<CH>;
+    // 32 units, 128 channels, at a time; wider rows: one half after the other
     const int lane = threadIdx.x & 31;
-    const uint32_t dst = stage + lane * 16, k0 = stage + M::k_lane(0), k1 = stage + M::k_lane(1);
-    const bool full = a.dh == kWidth;
-    unrolled<kPiece>([&](auto cn) {
-      constexpr int n = decltype(cn)::value, odd = n & 1;
-      const int j = n;
-      const int64_t off = a.aligned ? w.off + bytes_of(j, a.row) : __shfl_sync(0xffffffffu, w.off, j);
-      const char* src = (j == w.own ? w.k_new : w.k + off) + lane * 16;
-      const int bytes = (w.mask >> j) & 1 ? 16 : 0;
+    const uint32_t dst = stage + lane * 16, k0 = stage + k_lane(0), k1 = stage + k_lane(1);
+    // row n of K and V; `at`: bytes from k and v to it, constant
+    auto row = [&](auto cn, auto cat, const char* k, const char* v, int bytes) {
+      constexpr int n = decltype(cn)::value, at = decltype(cat)::value, odd = n & 1;
       unrolled<DC>([&](auto cd) {
         constexpr int d = decltype(cd)::value;
-        copy16<((n / 8) * KC + d * 8) * 512 + (n % 8 - odd) * 64, d * 512>(odd ? k1 : k0, src, full || d * 128 + lane * 4 < a.dh ? bytes : 0);
+        const int b = DC == 1 || d * 128 + lane * 4 < a.dh ? bytes : 0;
+        copy16<((n / 8) * KC + d * 8) * 512 + (n % 8 - odd) * 64, at + d * 512>(odd ? k1 : k0, k, b);
+        copy16<(2 * KC + n * DC + d) * 512, at + d * 512>(dst, v, b);
       });
-    });
-    unrolled<kPiece>([&](auto ci) {
-      constexpr int i = decltype(ci)::value;
-      const int j = i;
-      const int64_t off = a.aligned ? w.off + bytes_of(j, a.row) : __shfl_sync(0xffffffffu, w.off, j);
-      const char* src = (j == w.own ? w.v_new : w.v + off) + lane * 16;
-      const int bytes = (w.mask >> j) & 1 ? 16 : 0;
-      unrolled<DC>([&](auto cd) { constexpr int d = decltype(cd)::value; copy16<(2 * KC + i * DC + d) * 512, d * 512>(dst, src, full || d * 128 + lane * 4 < a.dh ? bytes : 0); });
+    };
+    if (a.aligned && w.mask == 0xffffu && w.own < 0 && a.dh == kWidth && a.row == kRowBytes / 16) {
+      const char *k = w.k + w.off + lane * 16, *v = w.v + w.off + lane * 16;
+      unrolled<kPiece>([&](auto cn) { row(cn, Const<decltype(cn)::value * kRowBytes>(), k, v, 16); });
+      return;
+    }
+    const bool there = lane * 4 < a.dh;                      // (of the first 128 channels)
+    unrolled<kPiece>([&](auto cn) {
+      constexpr int n = decltype(cn)::value;
+      const int64_t off = a.aligned ? w.off + bytes_of(n, a.row) : __shfl_sync(0xffffffffu, w.off, n);
+      row(cn, Const<0>(), (n == w.own ? w.k_new : w.k + off) + lane * 16, (n == w.own ? w.v_new : w.v + off) + lane * 16,
+          there && ((w.mask >> n) & 1) ? 16 : 0);
     });
   }
   __device__ __forceinline__ void use(const DecodeArgs& a, const unsigned char* stage, unsigned mask) {
@@ -956,7 +953,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
 
 // Shapes of the kernels: warps a CTA, stages of a warp's ring, CTAs per SM that fit.
 template <typename W, int WARPS> struct Shape {
-  static constexpr int kWarps = WARPS, kStages = W::kStage <= 4096 ? 6 : 3;
+  static constexpr int kWarps = WARPS, kStages = W::kStage <= 4096 && WARPS < 8 ? 6 : 3;
   static constexpr int kRings = kWarps * kStages * W::kStage;
   static constexpr int kPerSm = std::max(1, 227 * 1024 / (kRings + 2 * q_bytes<W>() + 5120));
   static constexpr int kItemsSmem = kRings + 2 * q_bytes<W>();
@@ -993,7 +990,7 @@ cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, 
   const long long units = (long long)batch * a.n_kv_heads * a.row_blocks;
   constexpr bool can_wide = W::kStage <= 8192;               // rings of eight warps fit an SM
   const bool wide = can_wide && units <= 4 * sm_count();
-  const int warps = wide ? 8 : S::kWarps, room = wide ? sm_count() : S::kPerSm * sm_count();
+  const int warps = wide ? 8 : S::kWarps, room = (wide ? Shape<W, 8>::kPerSm : S::kPerSm) * sm_count();
   int cluster = 1;
   while (cluster < kMaxCluster && units * cluster * 2 <= room && cluster * warps * kPiece < max_keys) cluster *= 2;
   if ((long long)max_keys <= (long long)cluster * warps * kPiece * kLongest) {
