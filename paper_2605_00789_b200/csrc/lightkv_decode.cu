@@ -709,14 +709,14 @@ constexpr int kItemsPerSlot = 2;
 constexpr int kMinBlocks = 4;         // of a part
 
 template <typename W> __host__ __device__ constexpr int part_floats() { return (W::kRows * (W::kWidth + 2) + 3) / 4 * 4; }   // rows on 16 bytes
-// With n blocks in all and parts of c >= n / most, fewer than `most` requests are cut (heads and row blocks counted apart), into fewer
+// With n blocks in all and parts of c > n / most, fewer than `most` requests are cut (heads and row blocks counted apart), into fewer
 // than 2 `most` parts, and there are fewer than `most` items more than requests.
 template <typename W> constexpr size_t items_bytes(int most) {
   return sizeof(JoinHeader) + (size_t(most) * sizeof(JoinRecord) + 255) / 256 * 256 + size_t(most) * 2 * part_floats<W>() * 4;
 }
 
-template <typename W, int WARPS, int NS, int PER_SM, int MOST>
-__global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const __grid_constant__ DecodeArgs a, int batch, JoinHeader* header,
+template <typename W, int WARPS, int NS, int PER_SM>
+__global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const __grid_constant__ DecodeArgs a, int batch, double inv_parts, JoinHeader* header,
                                                                          JoinRecord* records, float* parts) {
   // the warps' rings | query rows of this item and the next
   extern __shared__ __align__(128) unsigned char smem[];
@@ -754,7 +754,7 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
   unsigned total = 0;
 #pragma unroll
   for (int i = 0; i < WARPS; ++i) total += warp_blocks[i];
-  const unsigned chunk = max(unsigned(kMinBlocks), unsigned(((unsigned long long)total * heads + MOST - 1) / MOST));
+  const unsigned chunk = max(unsigned(kMinBlocks), unsigned(double((unsigned long long)total * heads) * inv_parts) + 1u);
   auto parts_of = [&](int n) { return n > 0 ? (blocks_of(n) + chunk - 1) / chunk : 1u; };
   // items, slots of cut requests and cut requests in front of the run
   int sums[3] = {0, 0, 0};
@@ -882,10 +882,10 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
 // The parts of a request that was cut: CTAs take one record after the other and `rows` rows of it; groups of threads take the parts
 // in turn.
 template <typename W>
-__global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs a, int rows, const JoinHeader* header,
+__global__ void __launch_bounds__(512) decode_join_kernel(const __grid_constant__ DecodeArgs a, int rows, const JoinHeader* header,
                                                           const JoinRecord* records, const float* parts) {
-  __shared__ float4 os[256];
-  __shared__ float tops[256], sums[256];
+  __shared__ float4 os[512];
+  __shared__ float tops[512], sums[512];
   constexpr int QUADS = W::kWidth / 4;
   grid_dependency_sync();
   const int n = header->n;
@@ -893,7 +893,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
   for (int i_rec = blockIdx.x; i_rec < n; i_rec += gridDim.x) {
     if (i_rec != int(blockIdx.x)) rec = records[i_rec];
     const int r0 = blockIdx.y * rows, outputs = min(rows, min(W::kRows, a.group - rec.head0 % a.group) - r0) * QUADS;
-    const int per_round = min(outputs, 256), groups = outputs > 0 ? 256 / per_round : 0, g = outputs > 0 ? threadIdx.x / per_round : 0;
+    const int per_round = min(outputs, 512), groups = outputs > 0 ? 512 / per_round : 0, g = outputs > 0 ? threadIdx.x / per_round : 0;
     const int used = min(groups, rec.parts);
     const float* first = parts + size_t(rec.slot) * part_floats<W>();
     for (int base = 0; base < outputs; base += per_round) {
@@ -1002,14 +1002,17 @@ cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, 
   JoinHeader* header = static_cast<JoinHeader*>(workspace);
   JoinRecord* records = reinterpret_cast<JoinRecord*>(header + 1);
   float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + sizeof(JoinHeader) + (size_t(S::kMost) * sizeof(JoinRecord) + 255) / 256 * 256);
-  auto kernel = decode_items_kernel<W, S::kWarps, S::kStages, S::kPerSm, S::kMost>;
+  // Parts of total / kMost blocks make up to one item more per request and head; where these are few, a little larger ones, so that
+  // no CTA is left with one item more than the others (75.3 -> 73.2 us for the two requests of the table).
+  const double inv_parts = 1.0 / (double)(units <= S::kMost / 4 ? S::kMost - units : S::kMost);
+  auto kernel = decode_items_kernel<W, S::kWarps, S::kStages, S::kPerSm>;
   cudaError_t e = ensure_dynamic_smem(kernel, S::kItemsSmem);
   if (e == cudaSuccess)
-    e = launch_kernel(kernel, dim3((unsigned)(units + S::kMost)), dim3(32 * S::kWarps), S::kItemsSmem, stream, 1, a, batch, header, records, parts);
+    e = launch_kernel(kernel, dim3((unsigned)(units + S::kMost)), dim3(32 * S::kWarps), S::kItemsSmem, stream, 1, a, batch, inv_parts, header, records, parts);
   // few requests have many parts each: a CTA joins one row of them
   const int per_cta = units <= 64 ? 1 : rows;
   if (e == cudaSuccess)
-    e = launch_kernel(decode_join_kernel<W>, dim3((unsigned)std::min<long long>(units, 2 * kSms), (rows + per_cta - 1) / per_cta), dim3(256), 0, stream, 1,
+    e = launch_kernel(decode_join_kernel<W>, dim3((unsigned)std::min<long long>(units, 2 * kSms), (rows + per_cta - 1) / per_cta), dim3(512), 0, stream, 1,
                       a, per_cta, header, records, parts);
   return e;
 }
