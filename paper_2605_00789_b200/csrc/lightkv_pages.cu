@@ -50,7 +50,7 @@ struct PageRows {
   long long* fresh_at;                 // exclusive sums of the new tokens asked for, and behind the last the whole
   unsigned *gone_at, *grow_at;         // exclusive sums of the pages given back and asked for
   int *held, *have, *need;             // tokens; pages held; pages afterwards (have and ~have where it was not served)
-  __host__ __device__ static constexpr size_t bytes(int batch) { return size_t(batch + 1) * 8 + size_t(batch) * 20; }
+  __host__ __device__ static constexpr size_t bytes(int batch) { return (size_t(batch + 1) * 8 + size_t(batch) * 20 + 15) / 16 * 16; }
   __device__ __forceinline__ PageRows(unsigned char* p, int batch) {
     fresh_at = reinterpret_cast<long long*>(p);
     gone_at = reinterpret_cast<unsigned*>(fresh_at + batch + 1);
@@ -308,13 +308,18 @@ __global__ void __launch_bounds__(kPageThreads) pages_plan_kernel(const __grid_c
 }
 
 __global__ void __launch_bounds__(256) pages_move_kernel(const __grid_constant__ PageArgs a) {
-  __shared__ __align__(8) unsigned char on_chip[PageRows::bytes(kPageRows)];
+  __shared__ __align__(16) unsigned char on_chip[PageRows::bytes(kPageRows)];
   grid_dependency_sync();
   unsigned char* from = a.workspace + 256;
   const PageTotals totals = *reinterpret_cast<const PageTotals*>(a.workspace);
   if (a.batch <= kPageRows) {
-    const int words = int(PageRows::bytes(a.batch) / 4);
-    for (int i = threadIdx.x; i < words; i += 256) reinterpret_cast<int*>(on_chip)[i] = reinterpret_cast<const int*>(from)[i];
+    const int pieces = int(PageRows::bytes(a.batch) / 16);   // (at most seven a thread, all asked for at once)
+#pragma unroll
+    for (int i = 0; i < int((PageRows::bytes(kPageRows) / 16 + 255) / 256); ++i)
+      if (int(threadIdx.x) + i * 256 < pieces)
+        tc::cp_async16(tc::smem_u32(on_chip) + (threadIdx.x + i * 256) * 16, from + (threadIdx.x + i * 256) * 16, 16);
+    tc::cp_async_commit();
+    tc::cp_async_wait<0>();
     __syncthreads();
     from = on_chip;
   }
