@@ -384,13 +384,15 @@ typedef struct {
 
 /* Bytes of scratch lightkv_assign_pages needs for `batch` requests; HOST only.  0 for a negative batch. */
 size_t lightkv_pages_workspace(int32_t batch);
-/* Errors: INVALID_ARG (NULL or overlapping buffers, sizes that are not positive, slot_stride without a slot map, ...), WORKSPACE. */
+/* Errors: INVALID_ARG (NULL or equal buffers, sizes that are not positive, slot_stride without a slot map, a table of more than
+ * 2^31 - 1 tokens a request, ...), UNSUPPORTED (2^31 entries in all tables and the stack), WORKSPACE, CUDA. */
 int lightkv_assign_pages(const lightkv_pages_args_t* args);
 
 /* Write the key and value rows of n_tokens new tokens to their slots of a paged cache; all heads of token t go to slot
  * slot_map[t].  A contiguous cache [B, H_kv, N, dh] is one with n_pages = B and page_size = N.  Negative slots are skipped
  * silently, slots behind the pool with LIGHTKV_STATUS_PAGE.  Slots must differ; of two equal ones either row may stand there
- * afterwards.  Sources and caches are disjoint. */
+ * afterwards.  Sources and caches are disjoint.  Errors: INVALID_ARG, UNSUPPORTED (head_dim > 256, more than 32767 16-byte
+ * units in a token's rows), CUDA. */
 typedef struct {
   uint32_t struct_size;            /* sizeof(lightkv_append_args_t) */
   int32_t  n_tokens;               /* >= 0 */
@@ -412,11 +414,16 @@ int lightkv_append_kv(const lightkv_append_args_t* args);
  *   out[b, h] = sum_j p_j V[b, h / (H / H_kv), j],  p = softmax_j(scale q[b, h] . K[b, h / (H / H_kv), j]),  j < n_keys[b]
  *   lse[b, h] = log sum_j exp(scale q . K_j)
  * computed in one pass over K and V.  Logits, sums and the accumulated rows are fp32; bf16 rows are rounded once, at the end.
- * A request with n_keys[b] <= 0 has a row of zeros and lse = -inf, and so has one whose logits are all -inf.
+ * A request with n_keys[b] <= 0 has a row of zeros and lse = -inf, and so has one whose logits are all -inf.  NaN and infinities
+ * go their way (an infinite bf16 value of a key with weight gives NaN: the weight is two summands); those of keys behind
+ * n_keys[b] do not.
  * k_new, v_new: rows of the token itself.  They stand for row n_keys[b] - 1 of the cache and are written there by the call.
  * Keys whose page number lies outside [0, n_pages) are left out (LIGHTKV_STATUS_PAGE); n_keys beyond the table's (or a
  * contiguous request's) rows is cut to them (LIGHTKV_STATUS_COUNT).  What the cache holds behind n_keys[b] is not read.
- * The workspace need not be cleared and may be shared by calls that are ordered on the device. */
+ * The workspace need not be cleared and may be shared by calls that are ordered on the device.
+ * Errors: INVALID_ARG (NULL, misaligned or equal buffers, strides below the row's width or negative, H % H_kv, a scale that is
+ * negative or not finite, ...), UNSUPPORTED (head_dim > 256, strides of 64 GB, more keys in all than 32-bit counters of 32 hold),
+ * WORKSPACE, CUDA. */
 typedef struct {
   uint32_t struct_size;            /* sizeof(lightkv_decode_args_t) */
   int32_t  batch;

@@ -1068,7 +1068,7 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
     if (s < 0 || s * el % 16) return LIGHTKV_ERR_INVALID_ARG;
     if (s * el / 16 > 0xffffffffll) return LIGHTKV_ERR_UNSUPPORTED;                          // strides of 64 GB and more
   }
-  if (a->row_stride < a->head_dim || a->q == a->out) return LIGHTKV_ERR_INVALID_ARG;
+  if (a->row_stride < a->head_dim || a->q == a->out || (a->k_new && a->k_cache == a->v_cache)) return LIGHTKV_ERR_INVALID_ARG;
   if (!aligned(a->workspace, 256) ||
       a->workspace_bytes < lightkv_decode_workspace(a->batch, a->n_q_heads, a->n_kv_heads, a->head_dim, a->dtype))
     return LIGHTKV_ERR_WORKSPACE;

@@ -71,7 +71,7 @@ def _pages_args(L, **kw):
     (dict(seq_len_out=None), -1), (dict(block_table=None), -1), (dict(free_pages=None), -1), (dict(n_free=None), -1),
     (dict(n_free_out=None), -1), (dict(workspace=None), -1), (dict(max_blocks=1 << 27), -1), (dict(slot_map=None), -1),
     (dict(n_slots=0), -1), (dict(slot_map=None, n_slots=0, slot_stride=1), -1), (dict(slot_map=0x80004), -1),
-    (dict(free_pages=0x40000), -1), (dict(workspace=0x1000080), -3), (dict(workspace_bytes=128), -3)])
+    (dict(free_pages=0x40000), -1), (dict(n_pages=2 ** 31 - 1), -2), (dict(workspace=0x1000080), -3), (dict(workspace_bytes=128), -3)])
 def test_assign_pages_refuses(L, kw, code):
     assert L.library().lightkv_assign_pages(C.byref(_pages_args(L, **kw))) == code
 
@@ -118,7 +118,8 @@ def _decode_args(L, **kw):
     (dict(page_size=-1), -1), (dict(max_blocks=0), -1), (dict(n_pages=0), -1), (dict(page_size=0), -1), (dict(max_keys=-1), -1),
     (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(q=0x1008), -1), (dict(out=0x1000), -1),
     (dict(row_stride=56), -1), (dict(row_stride=68), -1), (dict(q_head_stride=68), -1), (dict(workspace=0x1000010), -3),
-    (dict(workspace_bytes=16), -3), (dict(batch=1 << 27), -2)])
+    (dict(workspace_bytes=16), -3), (dict(batch=1 << 27), -2), (dict(page_stride=-2048), -1), (dict(page_stride=1 << 40), -2),
+    (dict(max_blocks=1 << 27, batch=1 << 9), -2), (dict(k_new=0x7000, v_new=0x8000, v_cache=0x2000), -1)])
 def test_decode_attention_refuses(L, kw, code):
     assert L.library().lightkv_decode_attention(C.byref(_decode_args(L, **kw))) == code
 
@@ -144,6 +145,26 @@ def test_the_binding_refuses_tensors_of_the_host(L):
     else:                                                                          # no current device to ask for
         with pytest.raises((RuntimeError, AssertionError, ValueError)):
             L.decode_attention(q, cache, cache.clone(), n, torch.empty_like(q), workspace=ws)
+
+
+# kernel -> registers a thread may have for the CTAs per SM that the launches count on; none of them spills
+LIMITS = {"decode_cluster_kernel<WarpBf16<2, 1>, 8, 3, 1>": 255, "decode_cluster_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
+          "decode_cluster_kernel<WarpBf16<1, 1>, 8, 3, 2>": 128, "decode_items_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
+          "decode_items_kernel<WarpBf16<2, 2>, 4, 3, 2>": 255, "decode_items_kernel<WarpBf16<1, 1>, 4, 6, 2>": 255}
+
+
+def test_registers_and_spills(tmp_path):
+    import re
+    log = subprocess.run([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")] + entry.NVCC_FLAGS + [
+        "-Xptxas", "-v", "-cubin", "-o", str(tmp_path / "out.cubin"), os.path.join(entry.CSRC, "lightkv_decode.cu")],
+        check=True, stdout=subprocess.PIPE, stderr=subprocess.STDOUT).stdout.decode()
+    log = subprocess.run(["c++filt"], input=log.replace("'_Z", "' _Z"), check=True, capture_output=True, text=True).stdout
+    log = log.replace("lkv::(anonymous namespace)::", "")
+    found = {k: (int(re.search(r"Used (\d+) registers", r).group(1)), int(re.search(r"(\d+) bytes spill loads", r).group(1)))
+             for k, r in re.findall(r"Compiling entry function '\s*(.*?)' for(.*?Used \d+ registers)", log, re.S)}
+    for kernel, limit in LIMITS.items():
+        (registers, spilled), = [v for k, v in found.items() if kernel + "(" in k]
+        assert registers <= limit and spilled == 0, (kernel, registers, spilled)
 
 
 def test_oracle_against_a_library_softmax():
@@ -431,11 +452,15 @@ EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, -1, 255, 300]
     (9, 1, 96, 16, "fp32", "head", False), (2, 2, 256, 16, "fp32", "token", True), (12, 2, 200, 32, "fp32", "head", True),
     (3, 3, 8, 1, "fp32", "head", True)])
 def test_decode_attention_at_the_edges(L, heads, kv_heads, dh, page, dtype, layout, new):
-    c = Decode(EDGES, heads, kv_heads, dh, page, dtype, layout, new)
+    # a table of 40000 keys a request: cut into items, joined by a second kernel; with the longest request announced: in clusters
+    c = Decode(EDGES, heads, kv_heads, dh, page, dtype, layout, new, width=40000 // page)
     rows = list(c.rows())
     before = (c.k.clone(), c.v.clone())
-    c.run(L)
-    c.check(rows)
+    for hint in (0, 300, 16, 1):
+        c.out.fill_(math.nan)
+        c.lse.fill_(math.nan)
+        c.run(L, max_keys=hint)
+        c.check(rows)
     # only the new rows have changed
     for cache, old, fresh in ((c.k, before[0], c.k_new), (c.v, before[1], c.v_new)):
         if new:
@@ -455,19 +480,19 @@ def test_decode_attention_at_the_edges(L, heads, kv_heads, dh, page, dtype, layo
 def test_decode_attention_batches(L, batch, heads, kv_heads, longest, dtype):
     if dtype == "fp32" and batch * longest * kv_heads > 60000:
         longest = max(1, 60000 // (batch * kv_heads))
+    seen = {}
     rng = np.random.default_rng(batch)
     lens = [int(v) for v in np.exp(rng.uniform(0, math.log(longest), batch))]
     lens[-1] = longest
-    c = Decode(lens, heads, kv_heads, 64, 16, dtype, new=batch % 2 == 0)
+    c = Decode(lens, heads, kv_heads, 64 if longest < 9000 else 128, 16, dtype, new=batch % 2 == 0, width=4000)
     rows = list(c.rows())
-    c.run(L)
-    c.check(rows)
-    first = c.out.clone(), c.lse.clone()
-    for hint in (longest, 0):                               # the hint chooses how the work is split, no more
+    for hint in (0, longest, 0, longest):                   # the hint chooses how the work is split, no more
         c.out.fill_(math.nan)
+        c.lse.fill_(math.nan)
         c.run(L, max_keys=hint)
         c.check(rows)
-    assert (c.out == first[0]).all() and (c.lse == first[1]).all()       # bit for bit, run after run
+        first = seen.setdefault(hint, (c.out.clone(), c.lse.clone()))
+        assert (c.out == first[0]).all() and (c.lse == first[1]).all()   # bit for bit, run after run
 
 
 @pytest.mark.gpu
@@ -631,6 +656,63 @@ def test_decode_attention_streams_graphs_and_a_shared_workspace(L):
     torch.cuda.synchronize()
     a.check(list(a.rows(lens)))
     b.check()
+
+
+@pytest.mark.gpu
+def test_decode_attention_two_streams_at_once(L):
+    """Calls that overlap on the GPU, each with its own workspace, in both forms."""
+    import torch
+    cs = [Decode([900, 40, 7, 2000], 8, 4, 64, 16, width=3000, seed=s) for s in range(4)]
+    rows = [list(c.rows()) for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    cs[0].run(L), cs[0].run(L, max_keys=2000)
+    for c in cs[1:]:
+        c.workspace = torch.full_like(cs[0].workspace, 255)
+    torch.cuda.synchronize()
+    for hint in (0, 2000):
+        for c in cs:
+            c.out.fill_(math.nan)
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for c, s in zip(cs, streams):
+                c.run(L, stream=s, max_keys=hint)
+        torch.cuda.synchronize()
+        for c, r in zip(cs, rows):
+            c.check(r)
+
+
+@pytest.mark.gpu
+def test_assign_pages_captured_steps_two_at_once(L):
+    """A captured step replayed on two streams with states of their own; lengths wanted without any held, in place."""
+    import torch
+    rng = np.random.default_rng(17)
+    states = []
+    for k in range(2):
+        lens = [int(v) for v in rng.integers(0, 60, 40)]
+        want = O.assign_pages(None, lens, 0, [[0] * 8 for _ in lens], list(rng.permutation(400)), 400, 16)
+        t = dict(seq=_i32(lens), table=_i32([[0] * 8 for _ in lens]), free=torch.zeros(400, dtype=torch.int32, device="cuda"), n=_i32([400]))
+        order = [int(v) for v in rng.permutation(400)]
+        t["free"].copy_(_i32(order))
+        ws = torch.full((L.pages_workspace_bytes(40),), 255, dtype=torch.uint8, device="cuda")
+        L.assign_pages(t["seq"], t["table"], t["free"], t["n"], page_size=16, workspace=ws)          # lengths in place of those wanted
+        want = O.assign_pages(None, lens, 0, [[0] * 8 for _ in lens], order, 400, 16)
+        assert t["seq"].tolist() == want["seq_len_out"] and t["table"].tolist() == want["table"] and int(t["n"]) == want["n_free"]
+        slots = torch.zeros(40, dtype=torch.int64, device="cuda")
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            L.assign_pages(t["seq"], t["table"], t["free"], t["n"], page_size=16, add=1, held=t["seq"], slot_map=slots, slot_stride=1, workspace=ws)
+        states.append((t, want, slots, stream, graph))
+    for _ in range(20):
+        for t, want, slots, stream, graph in states:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for t, want, slots, stream, graph in states:
+        for _ in range(20):
+            want = O.assign_pages(want["seq_len_out"], want["seq_len_out"], 1, want["table"], want["free_pages"], want["n_free"], 16, 40, 1)
+        assert t["seq"].tolist() == want["seq_len_out"] and t["table"].tolist() == want["table"] and int(t["n"]) == want["n_free"]
+        assert slots.tolist() == want["slot_map"]
 
 
 @pytest.mark.gpu
