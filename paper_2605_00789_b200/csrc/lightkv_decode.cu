@@ -224,10 +224,11 @@ struct WarpBf16 {
     constexpr int CH = kWidth / 8, R = 32 / CH, N = kPiece / R;              // units of a row; rows an instruction, instructions
     const int lane = threadIdx.x & 31, x = lane % CH, lr = lane / CH;
     const uint32_t dst = stage + lr * kRowBytes + ((x ^ lr) << 4);           // ^ ((n R) % 8 << 4), + n R kRowBytes
-    if (a.aligned && w.mask == 0xffffu && w.own < 0 && a.dh == kWidth) {
+    const bool there = x * 8 < a.dh;
+    if (a.aligned && w.mask == 0xffffu && w.own < 0) {
       const int64_t off = w.off + x * 16 + bytes_of(lr, a.row);
       const char *k = w.k + off, *v = w.v + off;
-      if (a.row == kRowBytes / 16) {
+      if (a.dh == kWidth && a.row == kRowBytes / 16) {
         unrolled<N>([&](auto cn) {
           constexpr int r0 = decltype(cn)::value * R;
           copy16<r0 * kRowBytes, r0 * kRowBytes>(dst ^ (r0 % 8 << 4), k, 16);
@@ -236,15 +237,14 @@ struct WarpBf16 {
       } else {
         unrolled<N>([&](auto cn) {
           constexpr int r0 = decltype(cn)::value * R;
-          copy16<r0 * kRowBytes, 0>(dst ^ (r0 % 8 << 4), k, 16);
-          copy16<r0 * kRowBytes + kHalf, 0>(dst ^ (r0 % 8 << 4), v, 16);
+          copy16<r0 * kRowBytes, 0>(dst ^ (r0 % 8 << 4), k, there ? 16 : 0);
+          copy16<r0 * kRowBytes + kHalf, 0>(dst ^ (r0 % 8 << 4), v, there ? 16 : 0);
           k += bytes_of(R, a.row);
           v += bytes_of(R, a.row);
         });
       }
       return;
     }
-    const bool there = x * 8 < a.dh;
     unrolled<N>([&](auto cn) {
       constexpr int r0 = decltype(cn)::value * R;
       const int j = r0 + lr;
@@ -971,16 +971,21 @@ cudaError_t launch_clusters(const DecodeArgs& a, long long units, int cluster, c
   return launch_kernel(kernel, dim3((unsigned)(units * cluster)), dim3(32 * WARPS), smem, stream, cluster, a, cluster);
 }
 
-// Which form a call takes.  Clusters where the longest request that the caller has announced gives a warp at most kLongest pieces: CTAs
-// of eight warps, as many to a request and head as there are SMs for, up to four waves of CTAs; CTAs of four, two on an SM, for more.
-// Items behind that: their plan and the join of their parts take about 6 us, but long requests are spread over all SMs.
+// Which form a call takes.  Clusters where the longest request that the caller has announced gives a warp at most kLongest pieces
+// (rounds): CTAs of eight warps, as many to a request and head as there are SMs for, up to four waves of CTAs; CTAs of four, two on an
+// SM, for more.  Clusters of eight only where they leave a third of the SMs free: 16 of them did not fit the GPU at once (2 x 600 keys,
+// 8 key heads 8.4 us against 5.6 with four).  Items behind that: their plan and the join of their parts take about 6 us, but long requests
+// are spread over all SMs.  With few CTAs (under 64 read slower than HBM allows), that pays earlier: a round takes 0.65 us against
+// 0.01 us for each of its CTAs at full bandwidth.
 //   us a call, bf16, head size 128 (64)       8 warps      4 warps      items
 //   1 x 404 keys, 32 heads                     5.2          6.2          9.4
+//   1 x 8000 keys, 8 key heads                 9.8
+//   1 x 16000 keys, 4 key heads               14.9                      12.6
 //   16 x 150 .. 1500, 8 key heads             13.4         14.3         18.9
 //   24 x 90 .. 2000, 8 key heads (64)         12.9         15.1         17.6
 //   48 x 301 .. 1399, 40 key heads             122          109          111
-//   96 x 0 .. 8192, 8 key heads                 99          113           94
-//   2 x 60000 .. 131072, 4 key heads           148          134           75
+//   96 x 0 .. 8192, 8 key heads                 99          113           95
+//   2 x 60000 .. 131072, 4 key heads           148          134           73
 constexpr int kLongest = 32;
 
 template <typename W>
@@ -992,8 +997,9 @@ cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, 
   const bool wide = can_wide && units <= 4 * sm_count();
   const int warps = wide ? 8 : S::kWarps, room = (wide ? Shape<W, 8>::kPerSm : S::kPerSm) * sm_count();
   int cluster = 1;
-  while (cluster < kMaxCluster && units * cluster * 2 <= room && cluster * warps * kPiece < max_keys) cluster *= 2;
-  if ((long long)max_keys <= (long long)cluster * warps * kPiece * kLongest) {
+  while (cluster < kMaxCluster && units * cluster * 2 <= (cluster < 4 ? room : room * 2 / 3) && cluster * warps * kPiece < max_keys) cluster *= 2;
+  const long long ctas = units * cluster, rounds = (max_keys + cluster * warps * kPiece - 1ll) / (cluster * warps * kPiece);
+  if (rounds <= kLongest && (ctas >= 64 || rounds * (64 - ctas) <= 350)) {
     if constexpr (can_wide)
       if (wide) return launch_clusters<W, 8>(a, units, cluster, stream);
     return launch_clusters<W, S::kWarps>(a, units, cluster, stream);
