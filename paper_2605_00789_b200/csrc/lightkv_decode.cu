@@ -43,6 +43,7 @@ struct DecodeArgs {
   float scale_log2;
   unsigned page_mul; int page_shift;   // key / page_size = (umulhi(key, page_mul) + key) >> page_shift for key < 2^31
   int aligned;                         // pieces do not straddle pages
+  int near_rows;                       // units of 16 bytes to any row fit 32 bits
 };
 
 using tc::cluster_sync;
@@ -245,6 +246,17 @@ struct WarpBf16 {
       }
       return;
     }
+    if (a.near_rows && w.mask == 0xffffu && w.own < 0) {     // (unaligned: a row's units by one shuffle)
+      const char *k = w.k + x * 16, *v = w.v + x * 16;
+      const uint32_t units = uint32_t(w.off >> 4);
+      unrolled<N>([&](auto cn) {
+        constexpr int r0 = decltype(cn)::value * R;
+        const uint64_t off = uint64_t(__shfl_sync(0xffffffffu, units, r0 + lr)) * 16;
+        copy16<r0 * kRowBytes, 0>(dst ^ (r0 % 8 << 4), k + off, there ? 16 : 0);
+        copy16<r0 * kRowBytes + kHalf, 0>(dst ^ (r0 % 8 << 4), v + off, there ? 16 : 0);
+      });
+      return;
+    }
     unrolled<N>([&](auto cn) {
       constexpr int r0 = decltype(cn)::value * R;
       const int j = r0 + lr;
@@ -396,6 +408,15 @@ struct WarpFp32 {
       return;
     }
     const bool there = lane * 4 < a.dh;                      // (of the first 128 channels)
+    if (a.near_rows && w.mask == 0xffffu && w.own < 0) {
+      const uint32_t units = uint32_t(w.off >> 4);
+      unrolled<kPiece>([&](auto cn) {
+        constexpr int n = decltype(cn)::value;
+        const uint64_t off = uint64_t(a.aligned ? units + n * a.row : __shfl_sync(0xffffffffu, units, n)) * 16 + lane * 16;
+        row(cn, Const<0>(), w.k + off, w.v + off, there ? 16 : 0);
+      });
+      return;
+    }
     unrolled<kPiece>([&](auto cn) {
       constexpr int n = decltype(cn)::value;
       const int64_t off = a.aligned ? w.off + bytes_of(n, a.row) : __shfl_sync(0xffffffffu, w.off, n);
@@ -1095,6 +1116,8 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   d.n_kv_heads = a->n_kv_heads; d.group = a->n_q_heads / a->n_kv_heads; d.dh = a->head_dim;
   page_divider(a->page_size > 0 ? (unsigned)a->page_size : 1u, &d.page_mul, &d.page_shift);
   d.aligned = a->page_size % kPiece == 0;
+  // units from the caches' start to the last row of a head, as the kernels reach it: pages (or rows of a request) and rows in a page
+  d.near_rows = ((double)d.page * (a->page_size > 0 ? a->n_pages : 0) + (double)d.row * (a->page_size > 0 ? a->page_size : a->max_keys)) < 4294967296.0;
   d.page_size = a->page_size; d.max_blocks = a->max_blocks; d.n_pages = a->n_pages;
   long long bound = a->page_size > 0 ? (long long)a->max_blocks * a->page_size : a->max_keys;
   if (bound > 0x7fffff00ll) bound = 0x7fffff00ll;                                            // keys are counted in 32 bits
