@@ -993,36 +993,38 @@ cudaError_t launch_clusters(const DecodeArgs& a, long long units, int cluster, c
 }
 
 // Which form a call takes.  Clusters where the longest request that the caller has announced gives a warp at most kLongest pieces
-// (rounds): CTAs of eight warps, as many to a request and head as there are SMs for, up to four waves of CTAs; CTAs of four, two on an
+// (rounds): CTAs that fill an SM, as many to a request and head as there are SMs for, up to four waves of CTAs; CTAs of four, two on an
 // SM, for more.  Clusters of eight only where they leave a third of the SMs free: 16 of them did not fit the GPU at once (2 x 600 keys,
 // 8 key heads 8.4 us against 5.6 with four).  Items behind that: their plan and the join of their parts take about 6 us, but long requests
 // are spread over all SMs.  With few CTAs (under 64 read slower than HBM allows), that pays earlier: a round takes 0.65 us against
 // 0.01 us for each of its CTAs at full bandwidth.
-//   us a call, bf16, head size 128 (64)       8 warps      4 warps      items
+//   us a call, bf16, head size 128 (64)       wide         4 warps      items
 //   1 x 404 keys, 32 heads                     5.2          6.2          9.4
 //   1 x 8000 keys, 8 key heads                 9.8
 //   1 x 16000 keys, 4 key heads               14.9                      12.6
 //   16 x 150 .. 1500, 8 key heads             13.4         14.3         18.9
-//   24 x 90 .. 2000, 8 key heads (64)         12.9         15.1         17.6
+//   24 x 90 .. 2000, 8 key heads (64)         12.1         15.1         17.6
 //   48 x 301 .. 1399, 40 key heads             122          109          111
 //   96 x 0 .. 8192, 8 key heads                 99          113           95
 //   2 x 60000 .. 131072, 4 key heads           148          134           73
 constexpr int kLongest = 32;
+// the wide CTAs' warps, whose rings fill an SM (24 x 90 .. 2000 keys of 64 channels: eight warps 13.5 us, sixteen 12.1)
+template <typename W> constexpr int wide_warps() { return W::kStage <= 4096 ? 16 : 8; }
 
 template <typename W>
 cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, cudaStream_t stream) {
   using S = Items<W>;
   a.row_blocks = (a.group + W::kRows - 1) / W::kRows;
   const long long units = (long long)batch * a.n_kv_heads * a.row_blocks;
-  constexpr bool can_wide = W::kStage <= 8192;               // rings of eight warps fit an SM
+  constexpr bool can_wide = W::kStage <= 8192;               // (rings of eight warps would not fit an SM)
   const bool wide = can_wide && units <= 4 * sm_count();
-  const int warps = wide ? 8 : S::kWarps, room = (wide ? Shape<W, 8>::kPerSm : S::kPerSm) * sm_count();
+  const int warps = wide ? wide_warps<W>() : S::kWarps, room = (wide ? Shape<W, wide_warps<W>()>::kPerSm : S::kPerSm) * sm_count();
   int cluster = 1;
   while (cluster < kMaxCluster && units * cluster * 2 <= (cluster < 4 ? room : room * 2 / 3) && cluster * warps * kPiece < max_keys) cluster *= 2;
   const long long ctas = units * cluster, rounds = (max_keys + cluster * warps * kPiece - 1ll) / (cluster * warps * kPiece);
   if (rounds <= kLongest && (ctas >= 64 || rounds * (64 - ctas) <= 350)) {
     if constexpr (can_wide)
-      if (wide) return launch_clusters<W, 8>(a, units, cluster, stream);
+      if (wide) return launch_clusters<W, wide_warps<W>()>(a, units, cluster, stream);
     return launch_clusters<W, S::kWarps>(a, units, cluster, stream);
   }
   const int rows = std::min(a.group, W::kRows);

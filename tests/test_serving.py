@@ -149,7 +149,8 @@ def test_the_binding_refuses_tensors_of_the_host(L):
 
 # kernel -> registers a thread may have for the CTAs per SM that the launches count on; none of them spills
 LIMITS = {"decode_cluster_kernel<WarpBf16<2, 1>, 8, 3, 1>": 255, "decode_cluster_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
-          "decode_cluster_kernel<WarpBf16<1, 1>, 8, 3, 2>": 128, "decode_items_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
+          "decode_cluster_kernel<WarpBf16<1, 1>, 16, 3, 1>": 128, "decode_cluster_kernel<WarpBf16<1, 2>, 16, 3, 1>": 128,
+           "decode_items_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
           "decode_items_kernel<WarpBf16<2, 2>, 4, 3, 2>": 255, "decode_items_kernel<WarpBf16<1, 1>, 4, 6, 2>": 255}
 
 
