@@ -974,7 +974,7 @@ __global__ void __launch_bounds__(512) decode_join_kernel(const __grid_constant_
 
 // Shapes of the kernels: warps a CTA, stages of a warp's ring, CTAs per SM that fit.
 template <typename W, int WARPS> struct Shape {
-  static constexpr int kWarps = WARPS, kStages = W::kStage <= 4096 && WARPS < 8 ? 6 : 3;
+  static constexpr int kWarps = WARPS, kStages = W::kStage <= 4096 && WARPS == 4 ? 6 : 3;
   static constexpr int kRings = kWarps * kStages * W::kStage;
   static constexpr int kPerSm = std::max(1, 227 * 1024 / (kRings + 2 * q_bytes<W>() + 5120));
   static constexpr int kItemsSmem = kRings + 2 * q_bytes<W>();
@@ -993,8 +993,9 @@ cudaError_t launch_clusters(const DecodeArgs& a, long long units, int cluster, c
 }
 
 // Which form a call takes.  Clusters where the longest request that the caller has announced gives a warp at most kLongest pieces
-// (rounds): CTAs that fill an SM, as many to a request and head as there are SMs for, up to four waves of CTAs; CTAs of four, two on an
-// SM, for more.  Clusters of eight only where they leave a third of the SMs free: 16 of them did not fit the GPU at once (2 x 600 keys,
+// (rounds): CTAs that fill an SM, as many to a request and head as there are SMs for, up to four waves of CTAs (two where requests are
+// short); CTAs of four warps, two on an SM, for more; CTAs of two warps for many requests of up to 256 keys (512, if they are more than
+// three to an SM), where a CTA's latency counts and not its bandwidth.  Clusters of eight only where they leave a third of the SMs free: 16 of them did not fit the GPU at once (2 x 600 keys,
 // 8 key heads 8.4 us against 5.6 with four).  Items behind that: their plan and the join of their parts take about 6 us, but long requests
 // are spread over all SMs.  With few CTAs (under 64 read slower than HBM allows), that pays earlier: a round takes 0.65 us against
 // 0.01 us for each of its CTAs at full bandwidth.
@@ -1006,8 +1007,11 @@ cudaError_t launch_clusters(const DecodeArgs& a, long long units, int cluster, c
 //   24 x 90 .. 2000, 8 key heads (64)         12.1         15.1         17.6
 //   48 x 301 .. 1399, 40 key heads             122          109          111
 //   96 x 0 .. 8192, 8 key heads                 99          113           95
+//   64 x 100 .. 800, 8 key heads              22.8         20.0
+//   64 x 60 .. 250, 8 key heads               16.0 (two warps: 10.1)
+//   61 x 1 .. 77, 8 key heads                 12.1 (two warps: 5.9)
 //   2 x 60000 .. 131072, 4 key heads           148          134           73
-constexpr int kLongest = 32;
+constexpr int kLongest = 32, kShort = 256;
 // the wide CTAs' warps, whose rings fill an SM (24 x 90 .. 2000 keys of 64 channels: eight warps 13.5 us, sixteen 12.1)
 template <typename W> constexpr int wide_warps() { return W::kStage <= 4096 ? 16 : 8; }
 
@@ -1016,8 +1020,10 @@ cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, 
   using S = Items<W>;
   a.row_blocks = (a.group + W::kRows - 1) / W::kRows;
   const long long units = (long long)batch * a.n_kv_heads * a.row_blocks;
+  // many short requests: CTAs of two warps, of which four share an SM
+  if (units > sm_count() && max_keys <= kShort * (units > 3 * sm_count() ? 2 : 1)) return launch_clusters<W, 2>(a, units, 1, stream);
   constexpr bool can_wide = W::kStage <= 8192;               // (rings of eight warps would not fit an SM)
-  const bool wide = can_wide && units <= 4 * sm_count();
+  const bool wide = can_wide && units <= (max_keys <= 1024 ? 2 : 4) * sm_count();
   const int warps = wide ? wide_warps<W>() : S::kWarps, room = (wide ? Shape<W, wide_warps<W>()>::kPerSm : S::kPerSm) * sm_count();
   int cluster = 1;
   while (cluster < kMaxCluster && units * cluster * 2 <= (cluster < 4 ? room : room * 2 / 3) && cluster * warps * kPiece < max_keys) cluster *= 2;

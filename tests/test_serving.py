@@ -150,7 +150,7 @@ def test_the_binding_refuses_tensors_of_the_host(L):
 # kernel -> registers a thread may have for the CTAs per SM that the launches count on; none of them spills
 LIMITS = {"decode_cluster_kernel<WarpBf16<2, 1>, 8, 3, 1>": 255, "decode_cluster_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
           "decode_cluster_kernel<WarpBf16<1, 1>, 16, 3, 1>": 128, "decode_cluster_kernel<WarpBf16<1, 2>, 16, 3, 1>": 128,
-           "decode_items_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
+          "decode_cluster_kernel<WarpBf16<2, 1>, 2, 3, 3>": 255, "decode_items_kernel<WarpBf16<2, 1>, 4, 3, 2>": 255,
           "decode_items_kernel<WarpBf16<2, 2>, 4, 3, 2>": 255, "decode_items_kernel<WarpBf16<1, 1>, 4, 6, 2>": 255}
 
 
@@ -494,6 +494,25 @@ def test_decode_attention_batches(L, batch, heads, kv_heads, longest, dtype):
         c.check(rows)
         first = seen.setdefault(hint, (c.out.clone(), c.lse.clone()))
         assert (c.out == first[0]).all() and (c.lse == first[1]).all()   # bit for bit, run after run
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads, kv_heads, dh, page, dtype, new", [
+    (4, 2, 128, 16, "bf16", True), (16, 1, 128, 7, "bf16", False), (5, 5, 64, 16, "bf16", True), (12, 1, 64, 1, "bf16", False), (9, 1, 256, 16, "bf16", True),
+    (3, 1, 96, 32, "bf16", False), (1, 1, 256, 24, "bf16", True), (2, 2, 128, 16, "fp32", True), (8, 1, 64, 7, "fp32", False), (4, 1, 256, 16, "fp32", True)])
+def test_decode_attention_many_short_requests(L, heads, kv_heads, dh, page, dtype, new):
+    """More (request, head) pairs than SMs, in CTAs of two warps (up to 256 keys, or 512), of four, and of more."""
+    rng = np.random.default_rng(dh)
+    for longest in (60, 256, 500):
+        lens = [int(v) for v in rng.integers(0, longest + 1, 470 // kv_heads)]
+        lens[0], lens[1], lens[2] = longest, 1, -5
+        c = Decode(lens, heads, kv_heads, dh, page, dtype, new=new)
+        rows = list(c.rows())
+        for hint in (0, 1100):
+            c.out.fill_(math.nan)
+            c.lse.fill_(math.nan)
+            c.run(L, max_keys=hint)
+            c.check(rows)
 
 
 @pytest.mark.gpu
