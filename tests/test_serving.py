@@ -624,22 +624,25 @@ def test_decode_attention_infinities_and_nan(L, dtype):
 
 
 @pytest.mark.gpu
-def test_decode_attention_offsets_past_32_bits(L):
-    """Pages more than 2^32 bytes (and 2^31 elements) behind the pool's start, odd token counts."""
+@pytest.mark.parametrize("page, dtype", [(16, "bf16"), (24, "bf16"), (24, "fp32")])
+def test_decode_attention_offsets_past_32_bits(L, page, dtype):
+    """Pages more than 2^32 bytes (and 2^31 elements) behind the pool's start, odd token counts, in both forms."""
     import torch
-    c = Decode([100, 37], 4, 2, 128, 16, new=True)
-    far = 600000                                            # pages of 8 KB: 4.9 GB
-    k, v = (torch.empty((far + 16, 2, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    c = Decode([100, 37], 4, 2, 128, page, dtype, new=True, width=2000)
+    far = 600000 if dtype == "bf16" else 400000            # pages of 8, 12, 24 KB: 4.9 to 9.8 GB
+    k, v = (torch.empty((far + 16, 2, page, 128), dtype=c.dt, device="cuda") for _ in range(2))
     n = c.k.shape[0]
     k[far:far + n], v[far:far + n] = c.k, c.v
     rows = list(c.rows())
     table = torch.where(c.table >= 0, c.table + far, c.table)
-    L.decode_attention(c.q, k, v, c.n_keys, c.out, block_table=table, lse=c.lse, k_new=c.k_new, v_new=c.v_new, status=c.status,
-                       workspace=torch.empty((L.decode_workspace_bytes(2, 4, 2, 128),), dtype=torch.uint8, device="cuda"))
-    c.check(rows)
+    for hint in (0, 100):
+        c.out.fill_(math.nan)
+        L.decode_attention(c.q, k, v, c.n_keys, c.out, block_table=table, lse=c.lse, k_new=c.k_new, v_new=c.v_new, status=c.status, max_keys=hint,
+                           workspace=torch.empty((L.decode_workspace_bytes(2, 4, 2, 128, L.BF16 if dtype == "bf16" else L.FP32),), dtype=torch.uint8, device="cuda"))
+        c.check(rows)
     for b, last in ((0, 99), (1, 36)):
-        assert (k[int(table[b, last // 16]), :, last % 16] == c.k_new[b]).all()
-    slots = torch.tensor([(far + 3) * 16 + 5, (far + 9) * 16], device="cuda")
+        assert (k[int(table[b, last // page]), :, last % page] == c.k_new[b]).all()
+    slots = torch.tensor([(far + 3) * page + 5, (far + 9) * page], device="cuda")
     L.append_kv(c.k_new, c.v_new, k, v, slots)
     assert (k[far + 3, :, 5] == c.k_new[0]).all() and (v[far + 9, :, 0] == c.v_new[1]).all()
 
