@@ -183,24 +183,26 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
 
-// DC: channels in units of 64; NH: query heads in units of 8
+// DC: channels in units of 64 (0: 32 channels); NH: query heads in units of 8
 template <int DC, int NH>
 struct WarpBf16 {
-  static constexpr int kRows = 8 * NH, kWidth = 64 * DC, KC = 4 * DC;        // KC: steps of 16 channels
+  static constexpr int kRows = 8 * NH, kWidth = DC ? 64 * DC : 32, KC = kWidth / 16;       // KC: steps of 16 channels
   static constexpr int kRowBytes = kWidth * 2, kHalf = kPiece * kRowBytes;
   static constexpr int kStage = 2 * kHalf;                   // bytes: K, then V
   uint32_t q[NH][KC][2];
   float o[NH][KC][4];                  // channels 16 t + g (and + 8), heads 2c, 2c + 1 of lane 4 g + c
   float m[NH][2], l[NH][2];            // heads 2c and 2c + 1: reference exponent; this lane's part of the sum
 
+  // unit x of row r lies at unit x ^ turn(r) of the row, so that a unit of eight rows in a row falls into all banks
+  static __device__ __forceinline__ int turn(int r) { return kWidth >= 64 ? r & 7 : r >> 1 & 3; }
   // the query rows as 16-byte units, permuted as the stages' are
-  static __device__ __forceinline__ uint32_t q_unit(int r, int x) { return r * kRowBytes + ((x ^ (r & 7)) << 4); }
+  static __device__ __forceinline__ uint32_t q_unit(int r, int x) { return r * kRowBytes + ((x ^ turn(r)) << 4); }
   __device__ __forceinline__ void load_q(const unsigned char* rows) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
       // matrices of 8 heads x 8 channels: channels 0, 8, 16, 24 of two steps
-      const uint32_t at = smem_u32(rows) + (h * 8 + (lane & 7)) * kRowBytes + (((lane >> 3) ^ (lane & 7)) << 4);
+      const uint32_t at = smem_u32(rows) + (h * 8 + (lane & 7)) * kRowBytes + (((lane >> 3) ^ turn(lane & 7)) << 4);
 #pragma unroll
       for (int kc = 0; kc < KC; kc += 2) {
         uint32_t f[4];
@@ -220,11 +222,11 @@ struct WarpBf16 {
       l[h][0] = l[h][1] = 0.f;
     }
   }
-  // Copy the piece in hand into the stage at `stage`: unit x of row r to r * kRowBytes + 16 (x ^ r % 8).
+  // Copy the piece in hand into the stage at `stage`.
   __device__ __forceinline__ void fetch(const DecodeArgs& a, const Walk& w, uint32_t stage) {
     constexpr int CH = kWidth / 8, R = 32 / CH, N = kPiece / R;              // units of a row; rows an instruction, instructions
     const int lane = threadIdx.x & 31, x = lane % CH, lr = lane / CH;
-    const uint32_t dst = stage + lr * kRowBytes + ((x ^ lr) << 4);           // ^ ((n R) % 8 << 4), + n R kRowBytes
+    const uint32_t dst = stage + lr * kRowBytes + ((x ^ turn(lr)) << 4);     // ^ ((n R) % 8 << 4), + n R kRowBytes
     const bool there = x * 8 < a.dh;
     if (a.aligned && w.mask == 0xffffu && w.own < 0) {
       const int64_t off = w.off + x * 16 + bytes_of(lr, a.row);
@@ -271,7 +273,7 @@ struct WarpBf16 {
     const int lane = threadIdx.x & 31, g = lane >> 2;
     const uint32_t at = smem_u32(stage);
     // K: matrices of 8 keys x 8 channels in the order (keys, channels) (0, 0), (8, 0), (0, 8), (8, 8)
-    const uint32_t ka = at + (lane & 15) * kRowBytes + (((lane >> 4) ^ (lane & 7)) << 4);
+    const uint32_t ka = at + (lane & 15) * kRowBytes + (((lane >> 4) ^ turn(lane & 7)) << 4);
     float s[NH][4], s2[NH][4];         // two chains of products
 #pragma unroll
     for (int h = 0; h < NH; ++h)
@@ -327,7 +329,7 @@ struct WarpBf16 {
       }
     }
     // V transposed: (channels, keys) (0, 0), (8, 0), (0, 8), (8, 8)
-    const uint32_t va = at + kHalf + ((lane & 7) + (lane >> 4 << 3)) * kRowBytes + (((lane >> 3 & 1) ^ (lane & 7)) << 4);
+    const uint32_t va = at + kHalf + ((lane & 7) + (lane >> 4 << 3)) * kRowBytes + (((lane >> 3 & 1) ^ turn(lane & 7)) << 4);
 #pragma unroll
     for (int t = 0; t < KC; ++t) {
       uint32_t f[4];
@@ -974,7 +976,7 @@ __global__ void __launch_bounds__(512) decode_join_kernel(const __grid_constant_
 
 // Shapes of the kernels: warps a CTA, stages of a warp's ring, CTAs per SM that fit.
 template <typename W, int WARPS> struct Shape {
-  static constexpr int kWarps = WARPS, kStages = W::kStage <= 4096 && WARPS == 4 ? 6 : 3;
+  static constexpr int kWarps = WARPS, kStages = W::kStage <= 2048 || (W::kStage <= 4096 && WARPS == 4) ? 6 : 3;
   static constexpr int kRings = kWarps * kStages * W::kStage;
   static constexpr int kPerSm = std::max(1, 227 * 1024 / (kRings + 2 * q_bytes<W>() + 5120));
   static constexpr int kItemsSmem = kRings + 2 * q_bytes<W>();
@@ -1056,8 +1058,8 @@ cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, 
 template <typename F>
 auto with_variant(int dtype, int group, int dh, F f) {
   if (dtype == LIGHTKV_BF16) {
-    if (group <= 8) return dh <= 64 ? f(WarpBf16<1, 1>()) : dh <= 128 ? f(WarpBf16<2, 1>()) : f(WarpBf16<4, 1>());
-    return dh <= 64 ? f(WarpBf16<1, 2>()) : dh <= 128 ? f(WarpBf16<2, 2>()) : f(WarpBf16<4, 2>());
+    if (group <= 8) return dh <= 32 ? f(WarpBf16<0, 1>()) : dh <= 64 ? f(WarpBf16<1, 1>()) : dh <= 128 ? f(WarpBf16<2, 1>()) : f(WarpBf16<4, 1>());
+    return dh <= 32 ? f(WarpBf16<0, 2>()) : dh <= 64 ? f(WarpBf16<1, 2>()) : dh <= 128 ? f(WarpBf16<2, 2>()) : f(WarpBf16<4, 2>());
   }
   if (dh <= 128) return group == 1 ? f(WarpFp32<1, 1>()) : group <= 4 ? f(WarpFp32<1, 4>()) : f(WarpFp32<1, 8>());
   return group == 1 ? f(WarpFp32<2, 1>()) : f(WarpFp32<2, 4>());
