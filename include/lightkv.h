@@ -354,7 +354,9 @@ int lightkv_compact_kv(const lightkv_plan_t* plan, const lightkv_kv_args_t* args
  * A request that wants more than max_blocks * page_size tokens is not served either (LIGHTKV_STATUS_COUNT); lengths held beyond
  * that, or an n_free outside [0, n_pages], are cut to it and raise the same bit.  Entries of block_table and free_pages must be
  * page numbers that occur once; one outside [0, n_pages) is passed on as it is, its tokens get no slot (LIGHTKV_STATUS_PAGE).
- * seq_len_out[b] is w_b, h_b for a request that was not served, and seq_len[b] for a place without a request.
+ * seq_len_out[b] is w_b, h_b for a request that was not served, and seq_len[b] for a place without a request.  The length alone
+ * does not tell that there is no room for the row of a new token: slots do, and with slot_stride = 1 their map is what
+ * lightkv_append_kv and lightkv_decode_attention take.
  * Slots: request b has max(w_b - h_b, 0) new tokens, served or not; slot_start[b] is their number in front of b.  The i-th one's
  * slot goes to slot_map[slot_start[b] + i], or, with slot_stride > 0, to slot_map[b * slot_stride + i] where i < slot_stride.
  * Every other entry of slot_map [n_slots], those of requests not served among them, becomes -1.  Tokens for whose slots there
@@ -417,7 +419,10 @@ int lightkv_append_kv(const lightkv_append_args_t* args);
  * A request with n_keys[b] <= 0 has a row of zeros and lse = -inf, and so has one whose logits are all -inf.  NaN and infinities
  * go their way (an infinite bf16 value of a key with weight gives NaN: the weight is two summands); those of keys behind
  * n_keys[b] do not.
- * k_new, v_new: rows of the token itself.  They stand for row n_keys[b] - 1 of the cache and are written there by the call.
+ * k_new, v_new: rows of the token itself.  They stand for row n_keys[b] - 1 of the cache and are written there by the call, so
+ * n_keys[b] has to count the new token: for a request that got no room for it, row n_keys[b] - 1 is its last old one.  slot_map
+ * says which these are: where slot_map[b] is negative, request b has no new row, nothing of it is written and all n_keys[b] rows
+ * are read from the cache.  (Of other entries only the sign counts.)  lightkv_assign_pages with slot_stride = 1 writes this array.
  * Keys whose page number lies outside [0, n_pages) are left out (LIGHTKV_STATUS_PAGE); n_keys beyond the table's (or a
  * contiguous request's) rows is cut to them (LIGHTKV_STATUS_COUNT).  What the cache holds behind n_keys[b] is not read.
  * The workspace need not be cleared and may be shared by calls that are ordered on the device.
@@ -444,6 +449,7 @@ typedef struct {
   const int32_t* n_keys;           /* DEVICE [B] */
   const void* k_new; const void* v_new;      /* DEVICE [B, H_kv, dh], both or neither */
   int64_t  new_batch_stride, new_head_stride;
+  const int64_t* slot_map;         /* DEVICE [B] or NULL (all requests have a new row); only with k_new */
   void*    out;                    /* DEVICE [B, H, dh]; does not overlap q */
   int64_t  out_batch_stride, out_head_stride;
   float*   lse;                    /* DEVICE [B, H] or NULL */

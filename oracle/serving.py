@@ -94,6 +94,14 @@ def cache_rows(cache, pages, n, page_size):
     return np.moveaxis(rows, 1, 0).astype(np.float64), there
 
 
+def with_new_row(k, v, k_new, v_new, slot=0):
+    """A request's rows [Hkv, n, dh] with those of the new token, [Hkv, dh], as the last ones; slot < 0: there is no new token."""
+    k, v = k.copy(), v.copy()
+    if slot >= 0 and k.shape[1] > 0:
+        k[:, -1], v[:, -1] = k_new, v_new
+    return k, v
+
+
 def attend(q, k, v, there, scale):
     """One request: q [H, dh], k / v [Hkv, n, dh] -> out [H, dh], lse [H], sum_j p_j |v_j| [H, dh], max_j sum_d |q_d k_jd| [H]."""
     heads, dh = q.shape

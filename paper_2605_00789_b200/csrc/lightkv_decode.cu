@@ -34,6 +34,7 @@ struct DecodeArgs {
   float* lse;
   const int* table;                    // nullptr: contiguous
   const int* n_keys;
+  const long long* slot_map;           // nullptr: every request has a new row where k_new is given
   uint32_t* status;
   int64_t lse_batch, lse_head;         // elements
   // strides in units of 16 bytes
@@ -105,7 +106,7 @@ struct Walk {
     k = a.k + at;
     v = a.v + at;
     k_new = v_new = nullptr;
-    if (a.k_new) {
+    if (a.k_new && (!a.slot_map || a.slot_map[b] >= 0)) {
       const int64_t own_at = bytes_of(b, a.new_batch) + bytes_of(hk, a.new_head);
       k_new = a.k_new + own_at;
       v_new = a.v_new + own_at;
@@ -1093,7 +1094,7 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   if (a->head_dim > 256) return LIGHTKV_ERR_UNSUPPORTED;
   if ((long long)a->batch * a->n_q_heads > 0x0fffffff) return LIGHTKV_ERR_UNSUPPORTED;      // CTAs of a launch
   if (!a->q || !a->k_cache || !a->v_cache || !a->n_keys || !a->out || !a->workspace) return LIGHTKV_ERR_INVALID_ARG;
-  if (!a->k_new != !a->v_new || a->page_size < 0 || a->max_keys < 0) return LIGHTKV_ERR_INVALID_ARG;
+  if (!a->k_new != !a->v_new || (a->slot_map && !a->k_new) || !aligned(a->slot_map, 8) || a->page_size < 0 || a->max_keys < 0) return LIGHTKV_ERR_INVALID_ARG;
   if (a->page_size > 0 ? !a->block_table || a->max_blocks <= 0 || a->n_pages <= 0 : a->max_keys <= 0) return LIGHTKV_ERR_INVALID_ARG;
   if (!isfinite(a->scale) || a->scale < 0.f) return LIGHTKV_ERR_INVALID_ARG;
   const void* ptrs[6] = {a->q, a->k_cache, a->v_cache, a->out, a->k_new, a->v_new};
@@ -1116,6 +1117,7 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   d.k_new = static_cast<const char*>(a->k_new); d.v_new = static_cast<const char*>(a->v_new);
   d.out = static_cast<char*>(a->out);
   d.lse = a->lse; d.n_keys = a->n_keys; d.status = a->status;
+  d.slot_map = reinterpret_cast<const long long*>(a->slot_map);
   d.table = a->page_size > 0 ? a->block_table : nullptr;
   auto units = [&](int64_t stride) { return (uint32_t)(stride * el / 16); };
   d.q_batch = units(a->q_batch_stride); d.q_head = units(a->q_head_stride);

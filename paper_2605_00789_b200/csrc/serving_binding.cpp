@@ -191,9 +191,9 @@ PyObject* guarded(F f) {
 
 PyObject* decode_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kwnames) {
   return guarded([&]() -> PyObject* {
-    static const Name names[] = {N_q, N_k_cache, N_v_cache, N_n_keys, N_out, N_workspace, N_block_table, N_lse, N_k_new, N_v_new, N_scale, N_max_keys,
-                                 N_status, N_stream};
-    const Args in("decode_attention", args, n, kwnames, names, 5, 1, 14);
+    static const Name names[] = {N_q, N_k_cache, N_v_cache, N_n_keys, N_out, N_workspace, N_block_table, N_lse, N_k_new, N_v_new, N_slot_map, N_scale,
+                                 N_max_keys, N_status, N_stream};
+    const Args in("decode_attention", args, n, kwnames, names, 5, 1, 15);
     lightkv_decode_args_t a = {};
     a.struct_size = sizeof(a);
     const at::Tensor& q = in.rows(N_q, 3, at::ScalarType::Undefined);
@@ -235,6 +235,10 @@ PyObject* decode_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObj
       Args::same(N_k_new, t.size(1), c.size(1), what[1]);
       Args::same(N_k_new, t.size(2), c.size(3), what[2]);
       a.k_new = k; a.v_new = v; a.new_batch_stride = t.stride(0); a.new_head_stride = t.stride(1);
+    }
+    if (in.get(N_slot_map)) {
+      if (!a.k_new) refuse(PyExc_ValueError, "'slot_map' comes with 'k_new' and 'v_new'");
+      a.slot_map = in.array<int64_t>(N_slot_map, at::kLong, q.size(0));
     }
     if (PyObject* s = in.get(N_scale)) {
       const double scale = PyFloat_AsDouble(s);
@@ -331,13 +335,14 @@ PyObject* bind(PyObject*, PyObject* args) {
 #define METHOD(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f))
 PyMethodDef kMethods[] = {
     {"decode_attention", METHOD(decode_attention), METH_FASTCALL | METH_KEYWORDS,
-     "decode_attention(q, k_cache, v_cache, n_keys, out, *, workspace, block_table=None, lse=None, k_new=None, v_new=None, scale=None,\n"
-     "                 max_keys=0, status=None, stream=None)\n\n"
+     "decode_attention(q, k_cache, v_cache, n_keys, out, *, workspace, block_table=None, lse=None, k_new=None, v_new=None,\n"
+     "                 slot_map=None, scale=None, max_keys=0, status=None, stream=None)\n\n"
      "lightkv_decode_attention.  q, out [B,H,dh]; n_keys [B] int32.  With block_table [B,max_blocks] int32 the caches are page pools\n"
      "[n_pages,H_kv,page_size,dh], else [B,H_kv,N,dh] (any strides with a contiguous last dimension, the same for K and V).\n"
      "workspace: a tensor of decode_workspace_bytes bytes; lse [B,H] fp32; k_new / v_new [B,H_kv,dh]: rows that stand for key\n"
-     "n_keys - 1 and are written to the cache; scale: default 1 / sqrt(dh); max_keys: an upper bound of n_keys (paged), by which the\n"
-     "split of the work is chosen; status [1] int32.  All tensors are on the current device."},
+     "n_keys - 1 and are written to the cache; slot_map [B] int64 (as assign_pages writes it with slot_stride=1): a request whose\n"
+     "entry is negative has no new row, and its n_keys rows are read as they stand; scale: default 1 / sqrt(dh); max_keys: an upper\n"
+     "bound of n_keys (paged), by which the split of the work is chosen; status [1] int32.  All tensors are on the current device."},
     {"append_kv", METHOD(append_kv), METH_FASTCALL | METH_KEYWORDS,
      "append_kv(k_new, v_new, k_cache, v_cache, slot_map, *, status=None, stream=None)\n\n"
      "lightkv_append_kv.  k_new, v_new [T,H_kv,dh]; caches [n_pages,H_kv,page_size,dh]; slot_map [T] int64, negative: skipped;\n"

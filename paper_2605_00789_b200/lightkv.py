@@ -117,7 +117,7 @@ class _DecodeArgs(C.Structure):
                 ("q_batch_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
                 ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64), ("block_table", C.c_void_p),
                 ("n_keys", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("new_batch_stride", C.c_int64),
-                ("new_head_stride", C.c_int64), ("out", C.c_void_p), ("out_batch_stride", C.c_int64),
+                ("new_head_stride", C.c_int64), ("slot_map", C.c_void_p), ("out", C.c_void_p), ("out_batch_stride", C.c_int64),
                 ("out_head_stride", C.c_int64), ("lse", C.c_void_p), ("lse_batch_stride", C.c_int64),
                 ("lse_head_stride", C.c_int64), ("status", C.c_void_p), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]

@@ -1,0 +1,154 @@
+"""The serving calls where one meets another, and at edges of their arguments: against the oracle, with the tolerances of
+tests/test_serving.py (its head derives them)."""
+import ctypes as C
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+
+import __graft_entry__ as entry
+from oracle import serving as O
+from tests.test_serving import Decode, _call_pages, _decode_args, _f64, _i32, _random, _random_pages
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def L():
+    entry.build()
+    import paper_2605_00789_b200 as pkg
+    return pkg
+
+
+# ------------------------------------------------------------------------------------------------------ without a GPU
+
+def _documented_loop():
+    """The body of the decoding loop that the README shows."""
+    block = re.search(r"```python\n(.*?)```", open(os.path.join(ROOT, "README.md")).read(), re.S).group(1)
+    body = block[block.index("for step in range(n):"):].split("\n", 1)[1]
+    return "\n".join(line[4:] for line in body.splitlines() if line.startswith("    "))
+
+
+def test_the_documented_loop_hands_the_slots_on():
+    calls = _documented_loop().splitlines()
+    assert [c.split("(")[0] for c in calls] == ["L.assign_pages", "L.decode_attention"]
+    assert all("slot_map=slots" in c and "status=status" in c for c in calls) and "slot_stride=1" in calls[0]
+
+
+@pytest.mark.parametrize("kw", [dict(slot_map=0x9000), dict(k_new=0x7000, v_new=0x8000, slot_map=0x9004)])
+def test_decode_attention_refuses_a_slot_map(L, kw):
+    """Without new rows, and where it is not aligned."""
+    assert L.library().lightkv_decode_attention(C.byref(_decode_args(L, **kw))) == -1
+
+
+def test_oracle_new_row():
+    k, v = np.zeros((2, 3, 4)), np.ones((2, 3, 4))
+    row = np.full((2, 4), 5.0)
+    kk, vv = O.with_new_row(k, v, row, 2 * row)
+    assert (kk[:, 2] == 5).all() and (vv[:, 2] == 10).all() and (kk[:, :2] == 0).all() and (k == 0).all()
+    kk, vv = O.with_new_row(k, v, row, row, -1)
+    assert (kk == k).all() and (vv == v).all()
+
+
+# ------------------------------------------------------------------------------------------------------------ on a GPU
+
+def _kernels(step):
+    """Kernels `step` launches."""
+    from bench import count_launches
+    return count_launches(step)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("width", [6, 9000])                # clusters; items and their join
+def test_the_documented_loop_where_pages_run_out(L, captured, width):
+    """Requests that get no page, or are at their table's end, keep every row bit for bit and attend to what they hold; the others
+    go on.  A page that comes free later serves the ones that waited."""
+    import torch
+    heads, kv_heads, dh, page = 8, 2, 64, 16
+    rng = np.random.default_rng(5)
+    # lengths; 1 and 2 need a page at once and there is one; 3 is at the end of a narrow table; 4 is no request; 0 needs its page at the third step
+    start = [30, 32, 48, 6 * page, -1, 5]
+    have = [-(-max(x, 0) // page) for x in start]
+    n_pages = sum(have) + 3
+    order, at, rows = [int(x) for x in rng.permutation(n_pages)], 0, []
+    for m in have:
+        rows.append(order[at:at + m] + [-1] * (width - m))
+        at += m
+    table, free, n_free = _i32(rows), _i32(order[at:] + [0] * at), _i32([1])
+    k, v = (_random(rng, (n_pages, kv_heads, page, dh), torch.bfloat16) for _ in range(2))
+    lens, status, slots = _i32(start), _i32([0]), torch.zeros(6, dtype=torch.int64, device="cuda")
+    q, k_new, v_new = (torch.empty((6, h, dh), dtype=torch.bfloat16, device="cuda") for h in (heads, kv_heads, kv_heads))
+    o = torch.empty_like(q)
+    ws = torch.zeros(max(L.pages_workspace_bytes(6), L.decode_workspace_bytes(6, heads, kv_heads, dh)), dtype=torch.uint8, device="cuda")
+    names = dict(L=L, lens=lens, table=table, free=free, n_free=n_free, slots=slots, status=status, ws=ws, q=q, k=k, v=v, o=o, k_new=k_new, v_new=v_new)
+    body = compile(_documented_loop(), "README", "exec")
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            exec(body, names)
+    state = dict(seq_len_out=list(start), table=rows, free_pages=free.tolist(), n_free=1)
+    waited = 0
+    for step in range(6):
+        if step == 3:                                       # two pages come back from elsewhere
+            state["free_pages"] = list(state["free_pages"])
+            state["free_pages"][:2] = order[at + 1:at + 3]
+            state["n_free"] = 2
+            free.copy_(_i32(state["free_pages"])), n_free.fill_(2)
+        for t, h in ((q, heads), (k_new, kv_heads), (v_new, kv_heads)):
+            t.copy_(_random(rng, (6, h, dh), torch.bfloat16))
+        status.zero_()
+        held = state["seq_len_out"]
+        state = O.assign_pages(held, held, 1, state["table"], state["free_pages"], state["n_free"], page, 6, 1)
+        want_k, want_v, _ = O.append_kv(_f64(k_new), _f64(v_new), _f64(k), _f64(v), state["slot_map"])
+        if captured:
+            graph.replay()
+        else:
+            exec(body, names)
+        torch.cuda.synchronize()
+        assert lens.tolist() == state["seq_len_out"] and slots.tolist() == state["slot_map"] and int(status) == state["status"]
+        np.testing.assert_array_equal(_f64(k), want_k)      # no old row has changed
+        np.testing.assert_array_equal(_f64(v), want_v)
+        for b, n in enumerate(lens.tolist()):
+            if n <= 0:
+                assert (o[b] == 0).all()
+                continue
+            waited += held[b] == n
+            (kk, there), (vv, _) = (O.cache_rows(c, table[b].tolist(), n, page) for c in (want_k, want_v))
+            ref, _, mass, span = O.attend(_f64(q[b]), kk, vv, there, dh ** -0.5)
+            rel = 2.0 ** -22 * (dh + 4) * span + 2.0 ** -20 + 2.0 ** -16 + 2.0 ** -22 * n
+            assert (np.abs(_f64(o[b]) - ref) <= 2.0 ** -8 * np.abs(ref) + rel[:, None] * mass).all(), (step, b)
+    assert waited >= 4 and lens.tolist()[2] > 48             # some waited, and were served later
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("page", [16, 7, 0])
+def test_decode_attention_new_rows_of_some_requests(L, dtype, page):
+    """A slot map of any signs, in both forms, paged and contiguous, with two blocks of query heads: a request without a new row
+    reads its last old one, and the cache keeps it."""
+    import torch
+    lens = [1, 16, 17, 33, 300, 0, 48, -1, 64, 2]
+    slots = [-1, -1, 5, -7, -1, -1, 0, 3, 2 ** 62, -2 ** 62]
+    c = Decode(lens, 40, 2, 64, page, dtype, new=True, width=40000 // page if page else None)
+    before = c.k.clone(), c.v.clone()
+    c.k_new.masked_fill_((torch.tensor(slots) < 0).cuda()[:, None, None], math.nan)          # what is not used may be anything
+    where = [None if n <= 0 else (int(c.table[b, (n - 1) // page]), (n - 1) % page) if page else (b, n - 1) for b, n in enumerate(lens)]
+    fresh = c.k_new, c.v_new
+    c.k_new = c.v_new = None
+    rows = [O.with_new_row(k, v, _f64(fresh[0][b]), _f64(fresh[1][b]), slots[b]) + (there,) for b, (k, v, there) in enumerate(c.rows())]
+    for x, y in zip((c.k, c.v), fresh):
+        for b, at in enumerate(where):
+            if at and slots[b] >= 0:
+                x[at[0], :, at[1]] = y[b]
+    after = c.k.clone(), c.v.clone()
+    c.k_new, c.v_new = fresh
+    for hint in (0, 300, 16) if page else (0,):
+        c.k.copy_(before[0]), c.v.copy_(before[1])
+        c.out.fill_(math.nan), c.lse.fill_(math.nan)
+        c.run(L, max_keys=hint, slot_map=torch.tensor(slots, device="cuda"))
+        c.check(rows)
+        for x, y in zip((c.k, c.v), after):
+            assert ((x == y) | (x.isnan() & y.isnan())).all()
