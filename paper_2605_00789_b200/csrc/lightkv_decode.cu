@@ -747,7 +747,7 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
   constexpr int THREADS = 32 * WARPS, kBlock = kPiece * WARPS, kRings = WARPS * NS * W::kStage, QUADS = W::kWidth / 4;
   __shared__ unsigned warp_blocks[WARPS];
   __shared__ int warp_sums[3][WARPS];
-  __shared__ int items_at[THREADS + 1], slots_at[THREADS], splits_at[THREADS], keys_at[THREADS];   // per run of requests
+  __shared__ int items_at[THREADS + 1], slots_at[THREADS], splits_at[THREADS + 1], keys_at[THREADS];   // per run of requests
   __shared__ Meeting<W, WARPS> meet;
   __shared__ __align__(16) unsigned char answer[16];
   __shared__ __align__(8) uint64_t answered;
@@ -807,7 +807,7 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
   if (t == 0) items_at[0] = 0;
   slots_at[t] = upto[1] - sums[1];
   splits_at[t] = upto[2] - sums[2];
-  if (blockIdx.x == 0 && t == THREADS - 1) header->n = upto[2];
+  if (t == THREADS - 1) splits_at[THREADS] = upto[2];
   __syncthreads();
   const int n_items = items_at[THREADS];
   if (int(blockIdx.x) >= n_items) return;
@@ -846,6 +846,8 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
     // the next item's copies are sent on their way before the parts of this one meet
     const bool more = item >= 0 && item < n_items;
     if (more) {
+      // by whoever has the first item: CTA 0 may have been cancelled before it started, like any other
+      if (item == 0 && t == 0) header->n = splits_at[THREADS];
       int r = 0;
 #pragma unroll
       for (int d = THREADS / 2; d; d >>= 1)

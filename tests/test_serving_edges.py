@@ -52,6 +52,21 @@ def test_oracle_new_row():
     assert (kk == k).all() and (vv == v).all()
 
 
+def _kernel_body(name):
+    """The text of a kernel of the attention, without comments."""
+    text = open(os.path.join(entry.CSRC, "lightkv_decode.cu")).read()
+    text = text[text.index(name + "(const __grid_constant__"):]
+    return re.sub(r"//.*", "", text[:text.index("\n}\n")])
+
+
+def test_no_cta_is_counted_on_to_start():
+    """Any CTA of the kernel that takes items may be cancelled by another before it starts: what the join reads is written by the
+    CTA that has the item, never by one of a certain number."""
+    body = _kernel_body("decode_items_kernel")
+    assert body.count("header->n =") == 1 and re.search(r"if \(item == 0 && t == 0\) header->n = splits_at\[THREADS\];", body)
+    assert re.findall(r"blockIdx\.x[^;]*;", body) == ["blockIdx.x) >= n_items) return;", "blockIdx.x;"]
+
+
 # ------------------------------------------------------------------------------------------------------------ on a GPU
 
 def _kernels(step):
@@ -108,9 +123,9 @@ def test_the_documented_loop_where_pages_run_out(L, captured, width):
         else:
             exec(body, names)
         torch.cuda.synchronize()
-        assert lens.tolist() == state["seq_len_out"] and slots.tolist() == state["slot_map"] and int(status) == state["status"]
         np.testing.assert_array_equal(_f64(k), want_k)      # no old row has changed
         np.testing.assert_array_equal(_f64(v), want_v)
+        assert lens.tolist() == state["seq_len_out"] and slots.tolist() == state["slot_map"] and int(status) == state["status"]
         for b, n in enumerate(lens.tolist()):
             if n <= 0:
                 assert (o[b] == 0).all()
