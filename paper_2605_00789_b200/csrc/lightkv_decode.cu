@@ -814,7 +814,7 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
 
   struct Item { int b, n, parts, part, slot, record, head0, n_rows; };
   static_assert(Partial<W>::kBytes <= W::kStage, "a stage holds a warp's partial rows");
-  bool bad = false, cut = false;
+  bool bad = false, cut = false, lost = false;
   uint32_t parity = 0;
   Walk w;
   W acc;
@@ -837,7 +837,8 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
         }
       });
       bad |= w.bad;
-      heard = tc::mbar_wait(&answered, parity, &abort_flag);
+      // each thread has its own limit: a warp agrees before its lanes shuffle, the CTA below (warps that heard have sent copies by then)
+      heard = __all_sync(0xffffffffu, tc::mbar_wait(&answered, parity, &abort_flag));
       parity ^= 1;
       item = heard ? tc::clc_canceled_cta(answer) : -1;
       tc::fence_proxy_async();         // the answer has been read before the next one is written
@@ -899,9 +900,14 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
       if (t == 0 && now.parts > 1 && now.part == 0) records[now.record] = {now.b, now.head0, now.parts, now.slot};
     }
     if (more) tc::cp_async_wait<NS - 1>();                   // the query rows are there
-    if (__syncthreads_or(!heard) || !more) break;
+    lost = __syncthreads_or(!heard);
+    if (lost || !more) break;
   }
   tc::cp_async_wait<0>();
+  if (lost && t == 0) {                // the answer is written to this CTA's memory: it gets as long again
+    abort_flag = 0;
+    tc::mbar_wait(&answered, parity ^ 1, &abort_flag);
+  }
   report(a, bad, cut);
 }
 

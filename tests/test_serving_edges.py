@@ -67,6 +67,20 @@ def test_no_cta_is_counted_on_to_start():
     assert re.findall(r"blockIdx\.x[^;]*;", body) == ["blockIdx.x) >= n_items) return;", "blockIdx.x;"]
 
 
+def test_a_wait_that_runs_out_ends_alike_for_a_warp_and_a_cta():
+    """Every thread has a limit of its own.  Lanes shuffle behind the wait, so a warp votes at once; the CTA votes before its next
+    turn, and stays until the answer that is still under way had its time."""
+    body = _kernel_body("decode_items_kernel")
+    wait = body.index("mbar_wait")
+    assert re.search(r"heard = __all_sync\(0xffffffffu, tc::mbar_wait\(&answered, parity, &abort_flag\)\);", body)
+    vote = body.index("lost = __syncthreads_or(!heard);")
+    assert wait < body.index("ring.start(") < vote < body.index("if (lost || !more) break;")
+    assert re.search(r"if \(lost && t == 0\) \{\s*abort_flag = 0;\s*tc::mbar_wait\(&answered, parity \^ 1, &abort_flag\);", body[vote:])
+    # between the wait and the vote a CTA's threads meet only where all of them do: at parts of an item that was begun by all
+    assert body[wait:vote].count("__syncthreads") == 1
+    assert body.index("if (open) {\n      unsigned char* own", wait) < body.index("__syncthreads", wait) < vote
+
+
 # ------------------------------------------------------------------------------------------------------------ on a GPU
 
 def _kernels(step):
