@@ -16,6 +16,7 @@
 
 #include <algorithm>
 
+#include "decode_join.cuh"
 #include "launch.h"
 #include "tc_common.cuh"
 
@@ -727,8 +728,6 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_cluster_kernel(cons
 // the launch of one that has not started and does its work.  (Fixed equal shares of all keys, cut wherever they end, 132 against
 // 95 us for 96 requests of 37 to 8192 keys: shares of many short requests take longer.)  The parts of a request that was cut go to
 // the workspace and are joined by decode_join_kernel.
-struct JoinRecord { int b, head0, parts, slot; };
-struct JoinHeader { int n; int pad[63]; };
 constexpr int kItemsPerSlot = 2;
 constexpr int kMinBlocks = 4;         // of a part
 
@@ -914,16 +913,17 @@ __global__ void __launch_bounds__(32 * WARPS, PER_SM) decode_items_kernel(const 
 // The parts of a request that was cut: CTAs take one record after the other and `rows` rows of it; groups of threads take the parts
 // in turn.
 template <typename W>
-__global__ void __launch_bounds__(512) decode_join_kernel(const __grid_constant__ DecodeArgs a, int rows, const JoinHeader* header,
-                                                          const JoinRecord* records, const float* parts) {
+__global__ void __launch_bounds__(512) decode_join_kernel(const __grid_constant__ DecodeArgs a, int batch, int most, int rows,
+                                                          const JoinHeader* header, const JoinRecord* records, const float* parts) {
   __shared__ float4 os[512];
   __shared__ float tops[512], sums[512];
   constexpr int QUADS = W::kWidth / 4;
   grid_dependency_sync();
-  const int n = header->n;
+  const int n = join_count(header->n, most);
   JoinRecord rec = records[blockIdx.x];                      // (beside the number; behind it: anything)
   for (int i_rec = blockIdx.x; i_rec < n; i_rec += gridDim.x) {
     if (i_rec != int(blockIdx.x)) rec = records[i_rec];
+    if (!joinable(rec, batch, a.n_kv_heads * a.group, 2 * most)) continue;
     const int r0 = blockIdx.y * rows, outputs = min(rows, min(W::kRows, a.group - rec.head0 % a.group) - r0) * QUADS;
     const int per_round = min(outputs, 512), groups = outputs > 0 ? 512 / per_round : 0, g = outputs > 0 ? threadIdx.x / per_round : 0;
     const int used = min(groups, rec.parts);
@@ -1059,7 +1059,7 @@ cudaError_t launch_form(DecodeArgs a, int batch, int max_keys, void* workspace, 
   const int per_cta = units <= 64 ? 1 : rows;
   if (e == cudaSuccess)
     e = launch_kernel(decode_join_kernel<W>, dim3((unsigned)std::min<long long>(units, 2 * kSms), (rows + per_cta - 1) / per_cta), dim3(512), 0, stream, 1,
-                      a, per_cta, header, records, parts);
+                      a, batch, S::kMost, per_cta, header, records, parts);
   return e;
 }
 

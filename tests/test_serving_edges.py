@@ -10,6 +10,7 @@ import pytest
 
 import __graft_entry__ as entry
 from oracle import serving as O
+from tests.test_kernel_units import _run
 from tests.test_serving import Decode, _call_pages, _decode_args, _f64, _i32, _random, _random_pages
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -79,6 +80,50 @@ def test_a_wait_that_runs_out_ends_alike_for_a_warp_and_a_cta():
     # between the wait and the vote a CTA's threads meet only where all of them do: at parts of an item that was begun by all
     assert body[wait:vote].count("__syncthreads") == 1
     assert body.index("if (open) {\n      unsigned char* own", wait) < body.index("__syncthreads", wait) < vote
+
+
+def test_records_that_were_never_written_are_not_joined(tmp_path):
+    """A CTA whose wait ran out leaves its record as the workspace had it.  Whatever 16 bytes are there, the rows that a join of
+    them would write and the parts it would read lie inside; what the kernel writes itself is joined."""
+    out = _run(tmp_path, r"""
+#include <stdio.h>
+#include <string.h>
+#include "decode_join.cuh"
+int main() {
+  unsigned long long x = 88172645463325252ull;
+  auto next = [&] { x ^= x << 13; x ^= x >> 7; x ^= x << 17; return x; };
+  long long bad = 0, kept = 0, joined = 0;
+  const int batches[] = {1, 3, 1 << 27}, groups[] = {1, 7, 20}, rows[] = {1, 4, 8, 16}, mosts[] = {296, 1776};
+  for (int batch : batches) for (int group : groups) for (int block : rows) for (int most : mosts) {
+    const int kv = 2, heads = kv * group, slots = 2 * most;
+    auto check = [&](const lkv::JoinRecord& r) {
+      if (!lkv::joinable(r, batch, heads, slots)) return;
+      ++joined;
+      const int last = group - r.head0 % group < block ? group - r.head0 % group : block;      // rows a join writes
+      bad += r.b < 0 || r.b >= batch || r.head0 < 0 || (long long)r.head0 + last > heads || last < 1;
+      bad += r.slot < 0 || r.parts < 1 || (long long)r.slot + r.parts > slots;
+    };
+    const int edges[] = {0, 1, -1, slots, slots - 1, heads - 1, heads, batch - 1, batch, 0x7fffffff, -0x7fffffff - 1};
+    for (int b : edges) for (int h : edges) for (int p : edges) for (int s : edges) check({b, h, p, s});
+    for (int i = 0; i < 20000; ++i) {
+      lkv::JoinRecord r;
+      unsigned long long w[2] = {next(), next()};
+      memcpy(&r, w, sizeof(r));
+      check(r);
+      check({r.b % batch, r.head0 % heads, r.parts % (slots + 2), r.slot % (slots + 2)});
+    }
+    for (int hk = 0; hk < kv; ++hk) for (int h0 = 0; h0 < group; h0 += block)
+      kept += !lkv::joinable({batch - 1, hk * group + h0, 2, slots - 2}, batch, heads, slots) || !lkv::joinable({0, h0, slots, 0}, batch, heads, slots);
+    const int counts[] = {0, 5, most, most + 1, 0x7fffffff, -1, -0x7fffffff - 1};
+    for (int n : counts) bad += lkv::join_count(n, most) < 0 || lkv::join_count(n, most) > most || (n >= 0 && n <= most && lkv::join_count(n, most) != n);
+  }
+  printf("%lld %lld %d\n", bad, kept, joined > 1000);
+}
+""")
+    assert out == ["0", "0", "1"]
+    body = _kernel_body("decode_join_kernel")
+    assert "join_count(header->n, most)" in body
+    assert body.index("records[i_rec]") < body.index("if (!joinable(") < body.index("rec.head0 %") < body.index("rec.parts") < body.index("rec.slot")
 
 
 # ------------------------------------------------------------------------------------------------------------ on a GPU
