@@ -417,8 +417,8 @@ int lightkv_append_kv(const lightkv_append_args_t* args);
  *   lse[b, h] = log sum_j exp(scale q . K_j)
  * computed in one pass over K and V.  Logits, sums and the accumulated rows are fp32; bf16 rows are rounded once, at the end.
  * A request with n_keys[b] <= 0 has a row of zeros and lse = -inf, and so has one whose logits are all -inf.  NaN and infinities
- * go their way (an infinite bf16 value of a key with weight gives NaN: the weight is two summands); those of keys behind
- * n_keys[b] do not.
+ * go their way (a logit of +inf gives NaN in out and, unless another is NaN, +inf in lse; an infinite bf16 value of a key with
+ * weight may give NaN: the weight is two summands); those of keys behind n_keys[b] do not.
  * k_new, v_new: rows of the token itself.  They stand for row n_keys[b] - 1 of the cache and are written there by the call, so
  * n_keys[b] has to count the new token: for a request that got no room for it, row n_keys[b] - 1 is its last old one.  slot_map
  * says which these are: where slot_map[b] is negative, request b has no new row, nothing of it is written and all n_keys[b] rows

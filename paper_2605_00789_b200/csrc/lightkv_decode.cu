@@ -12,6 +12,7 @@
 // come, 16-byte units permuted by the row's last three bits; ldmatrix reads K as it is and V transposed.  P is rounded to two
 // bf16 summands (hi + lo, 16 bits of mantissa): with one the rounding of P would be as large as the rounding of the output row.
 // tcgen05 would need 64 rows of query heads to save arithmetic that HBM hides.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -298,7 +299,8 @@ struct WarpBf16 {
         if (mask != 0xffffu && !((mask >> (g + (i >> 1) * 8)) & 1)) s[h][i] = -INFINITY;
         grows |= s[h][i] > m[h][i & 1] + 8.f;
       }
-    // The reference of a row is raised only where a logit exceeds it by 2^8: weights stay below 256, sums in range.
+    // The reference of a row is raised only where a logit exceeds it by 2^8: weights stay below 256, sums in range.  It stays finite:
+    // a logit of +inf has an infinite weight and sum (inf - inf would leave no number for lse).
     if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
       for (int h = 0; h < NH; ++h)
@@ -307,7 +309,7 @@ struct WarpBf16 {
           float top = fmaxf(s[h][e], s[h][2 + e]);
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-          top = fmaxf(top, m[h][e]);
+          top = fminf(fmaxf(top, m[h][e]), FLT_MAX);
           const float f = top == -INFINITY ? 1.f : exp2_approx(m[h][e] - top);
           m[h][e] = top;
           l[h][e] *= f;
@@ -463,7 +465,7 @@ struct WarpFp32 {
         float top = fmaxf(s[0][r], s[1][r]);
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        top = fmaxf(top, m[r]);
+        top = fminf(fmaxf(top, m[r]), FLT_MAX);
         const float f = top == -INFINITY ? 1.f : exp2_approx(m[r] - top);
         m[r] = top;
         if ((r & 3) == c) l[r >> 2] *= f;

@@ -226,3 +226,54 @@ def test_decode_attention_new_rows_of_some_requests(L, dtype, page):
         c.check(rows)
         for x, y in zip((c.k, c.v), after):
             assert ((x == y) | (x.isnan() & y.isnan())).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads", [2, 14])
+def test_decode_attention_infinite_logits_and_values(L, dtype, heads):
+    """+inf, -inf and NaN in keys and infinite values, at the first key, the last, in several pieces and several parts of a cut
+    request: out and lse as the formulas have them in 64 bits, and rows of other heads within their tolerance."""
+    import torch
+    lens = [40, 40, 40, 40, 3000, 3000, 3000, 40, 17, 40]
+    c = Decode(lens, heads, 2, 64, 16, dtype, width=2500)
+    c.q.abs_()
+    inf, nan = math.inf, math.nan
+    keys = [(0, 0, inf), (1, 39, inf), (2, 3, inf), (2, 20, inf), (3, 5, inf), (3, 38, nan), (4, 2999, inf), (5, 7, inf), (5, 1500, inf),
+            (5, 2990, -inf), (6, 1, inf), (6, 2800, nan), (8, 16, -inf)]
+    keys += [(7, j, -inf) for j in range(40) if j != 11] + [(7, 11, inf)]
+    for b, j, x in keys:
+        c.k[int(c.table[b, j // 16]), 0, j % 16, 9] = x
+    c.v[int(c.table[9, 1]), 0, 5, 3] = inf
+    c.v[int(c.table[9, 0]), 0, 7, 4] = -inf
+    q, rows = _f64(c.q), list(c.rows())
+
+    def near(out, lse, exact, n):
+        ref, ref_lse, mass, span = exact
+        d = 2.0 ** -23 * 68 * span
+        rel = 2 * d + 2.0 ** -20 + (2.0 ** -16 if dtype == "bf16" else 0) + 2.0 ** -22 * n
+        assert (np.abs(out - ref) <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(ref) + rel[:, None] * mass).all()
+        assert (np.abs(lse - ref_lse) <= d + 2.0 ** -20 + 2.0 ** -22 * n + 2.0 ** -22 * np.abs(ref_lse)).all()
+
+    for hint in (0, 3000, 40, 1):
+        c.out.fill_(nan), c.lse.fill_(nan)
+        c.run(L, max_keys=hint)
+        out, lse = _f64(c.out), _f64(c.lse)
+        assert int(c.status) == 0
+        for b, (k, v, _) in enumerate(rows):
+            for h in range(heads // 2):                     # heads that read the first key head
+                if b == 9:                                  # infinite values
+                    assert not np.isfinite(out[b, h, [3, 4]]).any() and np.isfinite(np.delete(out[b, h], [3, 4])).all() and np.isfinite(lse[b, h])
+                    if dtype == "fp32":
+                        assert out[b, h, 3] == inf and out[b, h, 4] == -inf
+                    continue
+                with np.errstate(invalid="ignore"):
+                    s = 0.125 * (k[0] @ q[b, h])
+                if b == 8:                                  # a key without weight
+                    near(out[b, h:h + 1], lse[b, h:h + 1], O.attend(q[b, h:h + 1], k[:1, :16], v[:1, :16], np.ones(16, bool), 0.125), 17)
+                    continue
+                assert np.isnan(out[b, h]).all(), (hint, b, h)
+                assert np.isnan(lse[b, h]) if np.isnan(s).any() else lse[b, h] == inf, (hint, b, h, lse[b, h])
+        half = heads // 2                                   # the other key head has nothing of it
+        for b, (k, v, there) in enumerate(rows):
+            near(out[b, half:], lse[b, half:], O.attend(q[b, half:], k[1:], v[1:], there, 0.125), lens[b])
