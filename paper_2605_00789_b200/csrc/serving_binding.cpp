@@ -153,6 +153,9 @@ struct Args {
   }
 };
 
+// The stride of dimension i; one that holds a single element is never stepped over, whatever stride it has: `alone` then.
+int64_t step(const at::Tensor& t, int i, int64_t alone = 0) { return t.size(i) > 1 ? t.stride(i) : alone; }
+
 int32_t float_type(const at::Tensor& t, Name id) {
   if (t.scalar_type() == at::kBFloat16) return LIGHTKV_BF16;
   if (t.scalar_type() == at::kFloat) return LIGHTKV_FP32;
@@ -206,9 +209,9 @@ PyObject* decode_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObj
     Args::same(N_k_cache, c.size(3), q.size(2), what[2]);
     a.batch = Args::size(N_q, q.size(0)); a.n_q_heads = Args::size(N_q, q.size(1)); a.head_dim = Args::size(N_q, q.size(2));
     a.n_kv_heads = Args::size(N_k_cache, c.size(1));
-    a.q = q.data_ptr(); a.q_batch_stride = q.stride(0); a.q_head_stride = q.stride(1);
-    a.out = out.data_ptr(); a.out_batch_stride = out.stride(0); a.out_head_stride = out.stride(1);
-    a.page_stride = c.stride(0); a.head_stride = c.stride(1); a.row_stride = c.stride(2);
+    a.q = q.data_ptr(); a.q_batch_stride = step(q, 0); a.q_head_stride = step(q, 1);
+    a.out = out.data_ptr(); a.out_batch_stride = step(out, 0); a.out_head_stride = step(out, 1);
+    a.page_stride = step(c, 0); a.head_stride = step(c, 1); a.row_stride = step(c, 2, c.size(3));
     a.n_keys = in.array<int32_t>(N_n_keys, at::kInt, q.size(0));
     a.max_keys = in.integer(N_max_keys, 0);
     if (in.get(N_block_table)) {
@@ -234,7 +237,7 @@ PyObject* decode_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObj
       Args::same(N_k_new, t.size(0), q.size(0), what[0]);
       Args::same(N_k_new, t.size(1), c.size(1), what[1]);
       Args::same(N_k_new, t.size(2), c.size(3), what[2]);
-      a.k_new = k; a.v_new = v; a.new_batch_stride = t.stride(0); a.new_head_stride = t.stride(1);
+      a.k_new = k; a.v_new = v; a.new_batch_stride = step(t, 0); a.new_head_stride = step(t, 1);
     }
     if (in.get(N_slot_map)) {
       if (!a.k_new) refuse(PyExc_ValueError, "'slot_map' comes with 'k_new' and 'v_new'");
@@ -267,11 +270,11 @@ PyObject* append_kv(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw
     const at::Tensor& t = in.pair(N_k_new, N_v_new, 3, first.scalar_type(), &k, &v);
     Args::same(N_k_new, t.size(1), c.size(1), "heads");
     Args::same(N_k_new, t.size(2), c.size(3), "channels");
-    a.k_new = k; a.v_new = v; a.new_token_stride = t.stride(0); a.new_head_stride = t.stride(1);
+    a.k_new = k; a.v_new = v; a.new_token_stride = step(t, 0); a.new_head_stride = step(t, 1);
     a.slot_map = in.array<int64_t>(N_slot_map, at::kLong, t.size(0));
     a.n_tokens = Args::size(N_k_new, t.size(0)); a.n_pages = Args::size(N_k_cache, c.size(0)); a.n_kv_heads = Args::size(N_k_cache, c.size(1));
     a.page_size = Args::size(N_k_cache, c.size(2)); a.head_dim = Args::size(N_k_cache, c.size(3));
-    a.page_stride = c.stride(0); a.head_stride = c.stride(1); a.row_stride = c.stride(2);
+    a.page_stride = step(c, 0); a.head_stride = step(c, 1); a.row_stride = step(c, 2, c.size(3));
     a.status = in.status();
     a.stream = in.stream();
     loaded();

@@ -277,3 +277,37 @@ def test_decode_attention_infinite_logits_and_values(L, dtype, heads):
         half = heads // 2                                   # the other key head has nothing of it
         for b, (k, v, there) in enumerate(rows):
             near(out[b, half:], lse[b, half:], O.attend(q[b, half:], k[1:], v[1:], there, 0.125), lens[b])
+
+
+def _odd(t, dims):
+    """The same elements, with strides of one element more than a row where a dimension has a single one."""
+    assert all(t.shape[d] == 1 for d in dims)
+    return t.as_strided(t.shape, [t.shape[-1] + 1 if d in dims else s for d, s in enumerate(t.stride())], t.storage_offset())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_strides_of_single_elements_do_not_matter(L, dtype):
+    """One request, one head, one page, one row a page or one token: the stride of that dimension may be anything."""
+    import torch
+    c = Decode([1], 1, 1, 64, 1, dtype, new=True, spare=0)
+    c.k_new, c.v_new = c.k_new.clone(), c.v_new.clone()
+    assert c.k.shape == (1, 1, 1, 64)
+    rows = list(c.rows())
+    c.q, c.out, c.k_new, c.v_new = (_odd(t, (0, 1)) for t in (c.q, c.out, c.k_new, c.v_new))
+    c.k, c.v = _odd(c.k, (0, 1, 2)), _odd(c.v, (0, 1, 2))
+    c.run(L)
+    c.check(rows)
+    assert (c.k[0, 0, 0] == c.k_new[0, 0]).all()
+    fresh = _odd(_random(np.random.default_rng(1), (1, 1, 64), c.dt), (0, 1))
+    L.append_kv(fresh, fresh, c.k, c.v, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    assert (c.k[0, 0, 0] == fresh[0, 0]).all() and (c.v[0, 0, 0] == fresh[0, 0]).all()
+    # contiguous, one request of several rows
+    c = Decode([9], 2, 1, 64, 0, dtype)
+    rows = list(c.rows())
+    c.q, c.out, c.k, c.v = _odd(c.q, (0,)), _odd(c.out, (0,)), _odd(c.k, (0, 1)), _odd(c.v, (0, 1))
+    c.run(L)
+    c.check(rows)
+    with pytest.raises(L.LightKVError):                     # a stride that counts is refused as before
+        L.decode_attention(torch.zeros((2, 2, 72), dtype=c.dt, device="cuda").as_strided((2, 2, 64), (145, 72, 1)), c.k.expand(2, -1, -1, -1),
+                           c.v.expand(2, -1, -1, -1), _i32([1, 1]), torch.zeros((2, 2, 64), dtype=c.dt, device="cuda"), workspace=c.workspace)
