@@ -441,6 +441,7 @@ typedef struct {
   int32_t  n_pages;                /* pages of the pool (paged) */
   int32_t  max_keys;               /* contiguous: rows of a request.  Paged: an upper bound of n_keys that the caller knows, or
                                       0; it only helps to choose how the work is split */
+  int32_t  key_bound;              /* contiguous: such an upper bound, or 0 (paged: not looked at) */
   const void* q;                   /* DEVICE [B, H, dh] */
   int64_t  q_batch_stride, q_head_stride;
   void* k_cache; void* v_cache;    /* DEVICE; written only where k_new is given */

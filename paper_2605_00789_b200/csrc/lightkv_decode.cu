@@ -1104,7 +1104,7 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   if (a->head_dim > 256) return LIGHTKV_ERR_UNSUPPORTED;
   if ((long long)a->batch * a->n_q_heads > 0x0fffffff) return LIGHTKV_ERR_UNSUPPORTED;      // CTAs of a launch
   if (!a->q || !a->k_cache || !a->v_cache || !a->n_keys || !a->out || !a->workspace) return LIGHTKV_ERR_INVALID_ARG;
-  if (!a->k_new != !a->v_new || (a->slot_map && !a->k_new) || !aligned(a->slot_map, 8) || a->page_size < 0 || a->max_keys < 0) return LIGHTKV_ERR_INVALID_ARG;
+  if (!a->k_new != !a->v_new || (a->slot_map && !a->k_new) || !aligned(a->slot_map, 8) || a->page_size < 0 || a->max_keys < 0 || a->key_bound < 0) return LIGHTKV_ERR_INVALID_ARG;
   if (a->page_size > 0 ? !a->block_table || a->max_blocks <= 0 || a->n_pages <= 0 : a->max_keys <= 0) return LIGHTKV_ERR_INVALID_ARG;
   if (!isfinite(a->scale) || a->scale < 0.f) return LIGHTKV_ERR_INVALID_ARG;
   const void* ptrs[6] = {a->q, a->k_cache, a->v_cache, a->out, a->k_new, a->v_new};
@@ -1148,7 +1148,8 @@ int lightkv_decode_attention(const lightkv_decode_args_t* a) {
   d.cap = (int)bound;
   const double scale = a->scale != 0.f ? a->scale : 1.0 / sqrt((double)a->head_dim);
   d.scale_log2 = (float)(scale * 1.4426950408889634);
-  if (a->max_keys > 0 && a->max_keys < bound) bound = a->max_keys;
+  const int announced = a->page_size > 0 ? a->max_keys : a->key_bound;
+  if (announced > 0 && announced < bound) bound = announced;
   const cudaError_t e = with_variant(a->dtype, d.group, d.dh, [&](auto v) {
     return launch_form<decltype(v)>(d, a->batch, (int)bound, a->workspace, static_cast<cudaStream_t>(a->stream));
   });

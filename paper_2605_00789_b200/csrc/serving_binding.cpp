@@ -223,6 +223,7 @@ PyObject* decode_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObj
       if (!a.page_size) refuse(PyExc_ValueError, "'k_cache' has pages without rows");
     } else {
       Args::same(N_k_cache, c.size(0), q.size(0), what[0]);
+      a.key_bound = a.max_keys;
       a.max_keys = Args::size(N_k_cache, c.size(2));
     }
     if (in.get(N_lse)) {
@@ -345,7 +346,7 @@ PyMethodDef kMethods[] = {
      "workspace: a tensor of decode_workspace_bytes bytes; lse [B,H] fp32; k_new / v_new [B,H_kv,dh]: rows that stand for key\n"
      "n_keys - 1 and are written to the cache; slot_map [B] int64 (as assign_pages writes it with slot_stride=1): a request whose\n"
      "entry is negative has no new row, and its n_keys rows are read as they stand; scale: default 1 / sqrt(dh); max_keys: an upper\n"
-     "bound of n_keys (paged), by which the split of the work is chosen; status [1] int32.  All tensors are on the current device."},
+     "bound of n_keys, by which the split of the work is chosen; status [1] int32.  All tensors are on the current device."},
     {"append_kv", METHOD(append_kv), METH_FASTCALL | METH_KEYWORDS,
      "append_kv(k_new, v_new, k_cache, v_cache, slot_map, *, status=None, stream=None)\n\n"
      "lightkv_append_kv.  k_new, v_new [T,H_kv,dh]; caches [n_pages,H_kv,page_size,dh]; slot_map [T] int64, negative: skipped;\n"

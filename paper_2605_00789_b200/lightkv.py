@@ -113,7 +113,7 @@ class _AppendArgs(C.Structure):
 class _DecodeArgs(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("page_size", C.c_int32),
-                ("max_blocks", C.c_int32), ("n_pages", C.c_int32), ("max_keys", C.c_int32), ("q", C.c_void_p),
+                ("max_blocks", C.c_int32), ("n_pages", C.c_int32), ("max_keys", C.c_int32), ("key_bound", C.c_int32), ("q", C.c_void_p),
                 ("q_batch_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p),
                 ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64), ("block_table", C.c_void_p),
                 ("n_keys", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p), ("new_batch_stride", C.c_int64),

@@ -44,6 +44,11 @@ def test_decode_attention_refuses_a_slot_map(L, kw):
     assert L.library().lightkv_decode_attention(C.byref(_decode_args(L, **kw))) == -1
 
 
+def test_decode_attention_refuses_a_negative_bound(L):
+    for kw in (dict(max_keys=-1), dict(page_size=0, max_keys=100, key_bound=-1), dict(key_bound=-1)):
+        assert L.library().lightkv_decode_attention(C.byref(_decode_args(L, **kw))) == -1
+
+
 def test_oracle_new_row():
     k, v = np.zeros((2, 3, 4)), np.ones((2, 3, 4))
     row = np.full((2, 4), 5.0)
@@ -311,3 +316,26 @@ def test_strides_of_single_elements_do_not_matter(L, dtype):
     with pytest.raises(L.LightKVError):                     # a stride that counts is refused as before
         L.decode_attention(torch.zeros((2, 2, 72), dtype=c.dt, device="cuda").as_strided((2, 2, 64), (145, 72, 1)), c.k.expand(2, -1, -1, -1),
                            c.v.expand(2, -1, -1, -1), _i32([1, 1]), torch.zeros((2, 2, 64), dtype=c.dt, device="cuda"), workspace=c.workspace)
+
+
+@pytest.mark.gpu
+def test_a_bound_of_the_keys_counts_for_contiguous_caches_too(L):
+    """Caches with room for many more rows than are in use: without a bound items and their join are launched, with one a cluster.
+    The bound chooses how the work is split and cuts nothing: a wrong one gives the same rows."""
+    import torch
+    # 6 requests and heads make 48 CTAs of 16 warps in clusters of eight: 40000 keys are 20 rounds of their warps, 64000 are 32, and items
+    # are taken from rounds * (64 - 48) > 350 on
+    for room, cases in ((40000, ((0, 1), (400, 1))), (64000, ((0, 2), (400, 1), (64000, 2), (70000, 2), (20, 1)))):
+        c = Decode([400, 37, 0], 4, 2, 64, 0, new=True)
+        k, v = (torch.full((3, 2, room, 64), math.nan, dtype=c.dt, device="cuda") for _ in range(2))
+        k[:, :, :c.k.shape[2]], v[:, :, :c.v.shape[2]] = c.k, c.v
+        rows = list(c.rows())
+        c.k, c.v = k, v
+        for bound, kernels in cases:
+            c.out.fill_(math.nan), c.lse.fill_(math.nan)
+            c.run(L, max_keys=bound)
+            c.check(rows)
+            assert _kernels(lambda: c.run(L, max_keys=bound)) == kernels, (room, bound)
+    paged = Decode([400, 37, 0], 4, 2, 64, 16, width=4000)
+    paged.run(L)
+    assert [_kernels(lambda: paged.run(L, max_keys=bound)) for bound in (0, 400)] == [2, 1]
