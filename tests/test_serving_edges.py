@@ -339,3 +339,16 @@ def test_a_bound_of_the_keys_counts_for_contiguous_caches_too(L):
     paged = Decode([400, 37, 0], 4, 2, 64, 16, width=4000)
     paged.run(L)
     assert [_kernels(lambda: paged.run(L, max_keys=bound)) for bound in (0, 400)] == [2, 1]
+
+
+@pytest.mark.gpu
+def test_the_smoke_run_takes_both_forms(L, monkeypatch):
+    kernels, call = [], L.decode_attention
+
+    def counted(*args, **kw):
+        kernels.append(_kernels(lambda: call(*args, **kw)))
+        call(*args, **kw)
+
+    monkeypatch.setattr(L, "decode_attention", counted)
+    entry._smoke_serving()
+    assert kernels == [2, 1]
