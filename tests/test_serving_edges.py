@@ -4,6 +4,7 @@ import ctypes as C
 import math
 import os
 import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -129,6 +130,17 @@ int main() {
     body = _kernel_body("decode_join_kernel")
     assert "join_count(header->n, most)" in body
     assert body.index("records[i_rec]") < body.index("if (!joinable(") < body.index("rec.head0 %") < body.index("rec.parts") < body.index("rec.slot")
+
+
+@pytest.mark.parametrize("source, kernels", [("lightkv_decode", 56), ("lightkv_pages", 4)])
+def test_no_serving_kernel_spills(tmp_path, source, kernels):
+    """Every instance that the library holds, as the compiler reports it."""
+    log = subprocess.run([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")] + entry.NVCC_FLAGS + [
+        "-Xptxas", "-v", "-cubin", "-o", str(tmp_path / "out.cubin"), os.path.join(entry.CSRC, source + ".cu")],
+        check=True, stdout=subprocess.PIPE, stderr=subprocess.STDOUT).stdout.decode()
+    found = re.findall(r"Compiling entry function '(\w+)' for.*?(\d+) bytes stack frame, (\d+) bytes spill stores, (\d+) bytes spill loads", log, re.S)
+    assert len(found) == kernels
+    assert [f for f in found if f[1:] != ("0", "0", "0")] == []
 
 
 # ------------------------------------------------------------------------------------------------------------ on a GPU
