@@ -214,6 +214,21 @@ def test_the_documented_loop_where_pages_run_out(L, captured, width):
     assert waited >= 4 and lens.tolist()[2] > 48             # some waited, and were served later
 
 
+# one request a thread up to 256, several up to 1024, chunks of 1024 behind that; one kernel up to 1024 requests and 4096 slots
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_slots, stride", [(4096, 0), (4097, 0), (0, 0), (2048, 2)])
+@pytest.mark.parametrize("batch", [255, 256, 257, 512, 513, 1024, 1025, 2048, 2049])
+def test_assign_pages_where_its_forms_meet(L, batch, n_slots, stride):
+    rng = np.random.default_rng(batch + n_slots)
+    for tight in (False, True):
+        case = _random_pages(rng, batch, 3, 5, tight)
+        want = O.assign_pages(**case, add=1, n_slots=n_slots, slot_stride=stride)
+        for in_place in (None, "held"):
+            got = _call_pages(L, **case, add=1, n_slots=n_slots, slot_stride=stride, in_place=in_place)
+            for key in want:
+                assert got[key] == want[key], (key, tight, in_place)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("page", [16, 7, 0])
