@@ -392,8 +392,8 @@ int lightkv_assign_pages(const lightkv_pages_args_t* args);
 
 /* Write the key and value rows of n_tokens new tokens to their slots of a paged cache; all heads of token t go to slot
  * slot_map[t].  A contiguous cache [B, H_kv, N, dh] is one with n_pages = B and page_size = N.  Negative slots are skipped
- * silently, slots behind the pool with LIGHTKV_STATUS_PAGE.  Slots must differ; of two equal ones either row may stand there
- * afterwards.  Sources and caches are disjoint.  Errors: INVALID_ARG, UNSUPPORTED (head_dim > 256, more than 32767 16-byte
+ * silently, slots behind the pool with LIGHTKV_STATUS_PAGE.  Slots must differ: of rows for the same slot, each 16-byte piece that
+ * stands there afterwards may be another one's.  Sources and caches are disjoint.  Errors: INVALID_ARG, UNSUPPORTED (head_dim > 256, more than 32767 16-byte
  * units in a token's rows), CUDA. */
 typedef struct {
   uint32_t struct_size;            /* sizeof(lightkv_append_args_t) */
@@ -424,7 +424,8 @@ int lightkv_append_kv(const lightkv_append_args_t* args);
  * says which these are: where slot_map[b] is negative, request b has no new row, nothing of it is written and all n_keys[b] rows
  * are read from the cache.  (Of other entries only the sign counts.)  lightkv_assign_pages with slot_stride = 1 writes this array.
  * Keys whose page number lies outside [0, n_pages) are left out (LIGHTKV_STATUS_PAGE); n_keys beyond the table's (or a
- * contiguous request's) rows is cut to them (LIGHTKV_STATUS_COUNT).  What the cache holds behind n_keys[b] is not read.
+ * contiguous request's) rows is cut to them (LIGHTKV_STATUS_COUNT), and a new row then replaces the last of them, unless slot_map[b]
+ * is negative.  What the cache holds behind n_keys[b] is not read.
  * The workspace need not be cleared and may be shared by calls that are ordered on the device.
  * Errors: INVALID_ARG (NULL, misaligned or equal buffers, strides below the row's width or negative, H % H_kv, a scale that is
  * negative or not finite, ...), UNSUPPORTED (head_dim > 256, strides of 64 GB, more keys in all than 32-bit counters of 32 hold),
@@ -440,7 +441,8 @@ typedef struct {
   int32_t  max_blocks;             /* row stride of block_table (paged) */
   int32_t  n_pages;                /* pages of the pool (paged) */
   int32_t  max_keys;               /* contiguous: rows of a request.  Paged: an upper bound of n_keys that the caller knows, or
-                                      0; it only helps to choose how the work is split */
+                                      0; it only helps to choose how the work is split, and does where a table is much wider
+                                      than its requests are long (0 stands for max_blocks * page_size) */
   int32_t  key_bound;              /* contiguous: such an upper bound, or 0 (paged: not looked at) */
   const void* q;                   /* DEVICE [B, H, dh] */
   int64_t  q_batch_stride, q_head_stride;

@@ -342,7 +342,7 @@ struct AppendArgs {
 };
 
 // A CTA copies `per_cta` tokens, all heads of K and V, four pieces in flight per thread.  Bound by HBM: 32768 rows of 8 heads x 128
-// channels 43.2 us, 6.2 TB/s of reads and writes (the copy rate measured for the card is 6.56); 64 rows 1.4 us, a launch.
+// channels 45.0 us, 6.0 TB/s of reads and writes (the copy rate measured for the card is 6.56); 64 rows 1.4 us, a launch.
 __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendArgs a) {
   grid_dependency_sync();
   const int first = blockIdx.x * a.per_cta, n = min(a.per_cta, a.n_tokens - first);

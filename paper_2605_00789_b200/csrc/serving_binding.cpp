@@ -345,8 +345,9 @@ PyMethodDef kMethods[] = {
      "[n_pages,H_kv,page_size,dh], else [B,H_kv,N,dh] (any strides with a contiguous last dimension, the same for K and V).\n"
      "workspace: a tensor of decode_workspace_bytes bytes; lse [B,H] fp32; k_new / v_new [B,H_kv,dh]: rows that stand for key\n"
      "n_keys - 1 and are written to the cache; slot_map [B] int64 (as assign_pages writes it with slot_stride=1): a request whose\n"
-     "entry is negative has no new row, and its n_keys rows are read as they stand; scale: default 1 / sqrt(dh); max_keys: an upper\n"
-     "bound of n_keys, by which the split of the work is chosen; status [1] int32.  All tensors are on the current device."},
+     "entry is negative has no new row, and its n_keys rows are read as they stand; scale: None or 0 for 1 / sqrt(dh); max_keys: an\n"
+     "upper bound of n_keys, by which the split of the work is chosen (0: all rows that the table or the cache has room for);\n"
+     "status [1] int32.  All tensors are on the current device.  No requests: nothing happens."},
     {"append_kv", METHOD(append_kv), METH_FASTCALL | METH_KEYWORDS,
      "append_kv(k_new, v_new, k_cache, v_cache, slot_map, *, status=None, stream=None)\n\n"
      "lightkv_append_kv.  k_new, v_new [T,H_kv,dh]; caches [n_pages,H_kv,page_size,dh]; slot_map [T] int64, negative: skipped;\n"
@@ -356,7 +357,8 @@ PyMethodDef kMethods[] = {
      "             n_free_out=None, slot_map=None, slot_start=None, slot_stride=0, status=None, stream=None)\n\n"
      "lightkv_assign_pages.  seq_len [B], block_table [B,max_blocks], free_pages [n_pages], n_free [1]: int32.  workspace: a tensor of\n"
      "pages_workspace_bytes bytes; held [B] int32; seq_len_out [B] (default: in place of held, or of seq_len where none is given);\n"
-     "n_free_out [1] (default: in place of n_free); slot_map [n_slots] int64; slot_start [B+1] int32; status [1] int32."},
+     "n_free_out [1] (default: in place of n_free); slot_map [n_slots] int64; slot_start [B+1] int32; status [1] int32.  A batch of\n"
+     "no requests is refused."},
     {"setup", METHOD(setup), METH_VARARGS, nullptr},
     {"bind", METHOD(bind), METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -34,7 +34,7 @@ def _documented_loop():
 
 
 def test_the_documented_loop_hands_the_slots_on():
-    calls = _documented_loop().splitlines()
+    calls = [c for c in re.split(r"\n(?=\S)", _documented_loop()) if c]
     assert [c.split("(")[0] for c in calls] == ["L.assign_pages", "L.decode_attention"]
     assert all("slot_map=slots" in c and "status=status" in c for c in calls) and "slot_stride=1" in calls[0]
 
@@ -153,8 +153,8 @@ def _kernels(step):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("captured", [False, True])
-@pytest.mark.parametrize("width", [6, 9000])                # clusters; items and their join
-def test_the_documented_loop_where_pages_run_out(L, captured, width):
+@pytest.mark.parametrize("width, longest", [(6, 0), (9000, 0), (9000, 200)])          # clusters; items and their join; clusters
+def test_the_documented_loop_where_pages_run_out(L, captured, width, longest):
     """Requests that get no page, or are at their table's end, keep every row bit for bit and attend to what they hold; the others
     go on.  A page that comes free later serves the ones that waited."""
     import torch
@@ -174,7 +174,7 @@ def test_the_documented_loop_where_pages_run_out(L, captured, width):
     q, k_new, v_new = (torch.empty((6, h, dh), dtype=torch.bfloat16, device="cuda") for h in (heads, kv_heads, kv_heads))
     o = torch.empty_like(q)
     ws = torch.zeros(max(L.pages_workspace_bytes(6), L.decode_workspace_bytes(6, heads, kv_heads, dh)), dtype=torch.uint8, device="cuda")
-    names = dict(L=L, lens=lens, table=table, free=free, n_free=n_free, slots=slots, status=status, ws=ws, q=q, k=k, v=v, o=o, k_new=k_new, v_new=v_new)
+    names = dict(L=L, longest=longest, lens=lens, table=table, free=free, n_free=n_free, slots=slots, status=status, ws=ws, q=q, k=k, v=v, o=o, k_new=k_new, v_new=v_new)
     body = compile(_documented_loop(), "README", "exec")
     if captured:
         graph = torch.cuda.CUDAGraph()
