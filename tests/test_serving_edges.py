@@ -27,7 +27,7 @@ def L():
 # ------------------------------------------------------------------------------------------------------ without a GPU
 
 def _documented_loop():
-    """The body of the decoding loop that the README shows."""
+    """The body of the decoding loop that the users' page shows."""
     block = re.search(r"```python\n(.*?)```", open(os.path.join(ROOT, "README.md")).read(), re.S).group(1)
     body = block[block.index("for step in range(n):"):].split("\n", 1)[1]
     return "\n".join(line[4:] for line in body.splitlines() if line.startswith("    "))
@@ -175,7 +175,7 @@ def test_the_documented_loop_where_pages_run_out(L, captured, width, longest):
     o = torch.empty_like(q)
     ws = torch.zeros(max(L.pages_workspace_bytes(6), L.decode_workspace_bytes(6, heads, kv_heads, dh)), dtype=torch.uint8, device="cuda")
     names = dict(L=L, longest=longest, lens=lens, table=table, free=free, n_free=n_free, slots=slots, status=status, ws=ws, q=q, k=k, v=v, o=o, k_new=k_new, v_new=v_new)
-    body = compile(_documented_loop(), "README", "exec")
+    body = compile(_documented_loop(), "documented loop", "exec")
     if captured:
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
