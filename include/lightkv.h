@@ -393,8 +393,8 @@ int lightkv_assign_pages(const lightkv_pages_args_t* args);
 /* Write the key and value rows of n_tokens new tokens to their slots of a paged cache; all heads of token t go to slot
  * slot_map[t].  A contiguous cache [B, H_kv, N, dh] is one with n_pages = B and page_size = N.  Negative slots are skipped
  * silently, slots behind the pool with LIGHTKV_STATUS_PAGE.  Slots must differ: of rows for the same slot, each 16-byte piece that
- * stands there afterwards may be another one's.  Sources and caches are disjoint.  Errors: INVALID_ARG, UNSUPPORTED (head_dim > 256, more than 32767 16-byte
- * units in a token's rows), CUDA. */
+ * stands there afterwards may be another one's.  Sources and caches are disjoint.  Errors: INVALID_ARG, UNSUPPORTED
+ * (head_dim > 256, more than 32767 16-byte units in a token's rows), CUDA. */
 typedef struct {
   uint32_t struct_size;            /* sizeof(lightkv_append_args_t) */
   int32_t  n_tokens;               /* >= 0 */
